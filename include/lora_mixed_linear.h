@@ -78,6 +78,7 @@ typedef enum {
 #define LML_MAX_ADAPTER_IDS 4096 /* adapter ids 0 .. this-1 can be published and resolved on the device */
 #define LML_DECODE_MAX_TOKENS 16 /* T <= this takes the bandwidth-bound decode kernel */
 #define LML_MAX_PROJECTIONS 4 /* projections one lora_mixed_linear_multi call can take */
+#define LML_MAX_NORM_WIDTH 16384 /* widest row that lml_block_norm takes */
 
 const char* lml_status_string(lml_status s);
 
@@ -269,6 +270,105 @@ lml_status lora_mixed_linear_backward_adapters(lml_table* t, lml_table* t_T, con
                                                const int32_t* seg_offsets, const int32_t* slot_ids,
                                                const int32_t* slot_ids_T, int G, float* dA, float* dB,
                                                void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Rows of activations for the training calls below: bf16, or an 8-bit checkpoint (Section 2.2: the background
+ * training task shares the GPU's memory with serving; what a backward pass wants kept is x of every layer).
+ *
+ * A checkpoint holds, per row and block of 32 columns, 8-bit values q and a power of two 2^(b - 127); it stands for
+ * q * 2^(b - 127), exact in bf16.  The formats are those of the OCP Microscaling specification:
+ *   LML_ROWS_INT8  q = -127 ... 127, b the binade of the block's largest value less 6 (MXINT8): steps of 1/64 of that binade.
+ *   LML_ROWS_E4M3  q an FP8 E4M3 number, b the least with amax <= 448 * 2^(b - 127) (MXFP8): four significant bits.
+ * Rounded to nearest even, off by half a step at most (E4M3: 3.3e38 and more become 3.19e38, the next would be 2^128).  b >= 0 (INT8), >= 3 (E4M3): blocks below about 2^-120 lose their
+ * smallest values.  A block that holds Inf or NaN has b = 255 and reads back as NaN.
+ * data:   uint8 [T][pitch], pitch = d rounded up to a multiple of 32, zeros behind column d.
+ * scales: uint8 [ceil(d / 128)][T][4]: b of the four blocks of 128 columns (0 for blocks behind the last).
+ * Both are device memory of the caller's, 16-byte aligned, of lml_checkpoint_data_bytes(T, d) and
+ * lml_checkpoint_scale_bytes(T, d) bytes (0 for invalid arguments).  LML_ROWS_BF16: data is bf16 [T][d], scales is NULL.
+ */
+#define LML_ROWS_BF16 0
+#define LML_ROWS_INT8 1
+#define LML_ROWS_E4M3 2
+typedef struct {
+    void* data;
+    void* scales;
+    int format; /* LML_ROWS_* */
+} lml_rows;
+size_t lml_checkpoint_data_bytes(int T, int d);
+size_t lml_checkpoint_scale_bytes(int T, int d);
+
+/*
+ * lml_checkpoint_store / lml_checkpoint_load — bf16 [T][d] to a checkpoint (kept->format INT8 or E4M3) and back.
+ * d: a positive multiple of 8.  One launch each; T == 0 returns without one.  device: the CUDA device of the buffers.
+ * Errors: INVALID_ARG, CUDA.
+ */
+lml_status lml_checkpoint_store(int device, const void* x, int T, int d, const lml_rows* kept, void* stream);
+lml_status lml_checkpoint_load(int device, const lml_rows* kept, int T, int d, void* x, void* stream);
+
+/*
+ * lora_mixed_linear_backward_adapters_rows — the adapter gradients with x kept as rows of any of the formats above.
+ *   dA[slot][j][k] (+)= s sum_t (dy.B)[t][j] x[t][k],   dB[slot][n][j] (+)= s sum_t dy[t][n] (x.A^T)[t][j]
+ * as in lora_mixed_linear_backward_adapters, with x the values that the rows stand for.  Two launches on the tensor cores; the two
+ * small products are kept to 16 bits beyond the leading one instead of being rounded to bf16, so dA and dB carry fp32 sums of
+ * products that are exact to about 2^-17.  The order of the sums is fixed by the sizes, the segments and the bindings: the same call gives the same bits.
+ * accumulate != 0: rows j < rank of the slots in use are added to.  accumulate == 0: rows j < rank of EVERY live slot of t are
+ * written, zeros where the batch has no token of it (a step's first micro-batch then needs no zeroed buffers).  Rows j >= rank
+ * and slots without an adapter are left as they are either way.
+ * A segment takes part when its two slots hold adapters of one rank; one that names only one of them, a free slot or another
+ * rank adds nothing and sets LML_FLAG_BAD_SLOT (of t_T where t's slot is fine).  Malformed seg_offsets: LML_FLAG_BAD_OFFSETS,
+ * nothing is added.  A token's Inf or NaN reaches the gradients of its own adapter only.
+ * x, dy: rows in segment order (no perm), 16-byte aligned.  G >= 1.  dA, dB must not overlap x or dy.
+ * workspace: device, 256-byte aligned, lml_backward_rows_workspace_bytes(t, T, G) bytes.  Errors: INVALID_ARG, WORKSPACE, CUDA.
+ */
+size_t lml_backward_rows_workspace_bytes(const lml_table* t, int max_tokens, int max_segments);
+lml_status lora_mixed_linear_backward_adapters_rows(lml_table* t, lml_table* t_T, const lml_rows* x, const void* dy, int T,
+                                                    const int32_t* seg_offsets, const int32_t* slot_ids,
+                                                    const int32_t* slot_ids_T, int G, float* dA, float* dB, int accumulate,
+                                                    void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * lml_block_norm — what stands between the projections of two blocks of a decoder: the norm of the block's output o, its
+ * gate, the residual sum, and the next block's norm, which makes the x that the layer reads.  Per row of d values
+ *     n  = o * (mean(o^2) + eps)^-1/2 * w_post          (w_post NULL: n = o)
+ *     h' = h + scale * gate * n                         (rounded to bf16, as the residual stream is kept)
+ *     x  = h' * (mean(h'^2) + eps)^-1/2 * w_pre
+ * in fp32 between the roundings of h' and x.  The weights and the channel gate stand in a descriptor that a program keeps per block
+ * (device bf16 [d]; NULL: none; the struct is read during the call only, the weights when the work runs):
+ */
+typedef struct {
+    int d;          /* a multiple of 8, <= LML_MAX_NORM_WIDTH */
+    float eps;      /* > 0 */
+    float scale;    /* the residual scale */
+    const void* w_post;
+    const void* w_pre;
+    const void* gate;
+} lml_block_norm_desc;
+/*
+ * h, o: device bf16 [T][d].  o NULL: no block before (h' = h; w_post and gate are not read, h_new must be NULL).
+ * gate_rows: NULL, or a gate of its own for every token, bf16 [T][d] (the descriptor's gate is NULL then).
+ * h_new, x: bf16 [T][d] outputs, either may be NULL; without w_pre there is no x (x and x_kept NULL).  x_kept, h_kept: NULL, or
+ * checkpoints of x and of h' written in the same pass, bit for bit what lml_checkpoint_store makes of them.
+ * An output may be the buffer of an input of its shape (h_new = h, say), but not overlap it otherwise.  A row's results follow from the
+ * row and, in the order of its sums, from T and d.  One launch; T == 0 returns without one.  Errors: INVALID_ARG, CUDA.
+ */
+lml_status lml_block_norm(int device, const lml_block_norm_desc* desc, int T, const void* h, const void* o, const void* gate_rows,
+                          void* h_new, void* x, const lml_rows* x_kept, const lml_rows* h_kept, void* stream);
+/*
+ * lml_block_norm_backward — its gradients.  Given dx and dh_new (the gradients of x and h'; bf16 [T][d]; NULL: zero, not both),
+ * and h' and o as the forward pass kept them (bf16 or checkpoints; the gradients are those at the values that they stand for):
+ *   dh   [T][d]  gradient of h (= the whole gradient of h')         d_o  [T][d]  gradient of o
+ *   dw_pre, dw_post, dgate  float32 [d], ADDED to: the sums over the tokens; NULL: not wanted (frozen norms)
+ *   dgate_rows  bf16 [T][d], written: gradient of gate_rows
+ * h_new may be NULL without dx, o NULL where the forward call had none (then d_o, dw_post, dgate, dgate_rows are NULL).
+ * An output NULL is not made.  Buffers may be shared as above (dh = dh_new, d_o = dx, say).  Sums over tokens are added in an order that
+ * T and d fix.  One launch, two where sums are wanted; those need workspace: lml_block_norm_workspace_bytes(device, T, d), 256-byte aligned.
+ * Errors: INVALID_ARG, WORKSPACE, CUDA.
+ */
+size_t lml_block_norm_workspace_bytes(int device, int T, int d);
+lml_status lml_block_norm_backward(int device, const lml_block_norm_desc* desc, int T, const lml_rows* h_new, const lml_rows* o,
+                                   const void* gate_rows, const void* dx, const void* dh_new, void* dh, void* d_o, float* dw_pre,
+                                   float* dw_post, float* dgate, void* dgate_rows, void* workspace, size_t workspace_bytes,
+                                   void* stream);
 
 /*
  * lora_mixed_linear_tokens — segmentation and layer in one call, for callers that hold one slot id

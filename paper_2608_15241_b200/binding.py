@@ -34,7 +34,24 @@ EXPORTS = ("lml_status_string", "lml_table_create", "lml_table_destroy", "regist
            "lml_segment_tokens_adapters", "lora_mixed_linear_adapters",
            "lml_dual_workspace_bytes", "lora_mixed_linear_dual", "register_adapter_transposed",
            "lml_backward_workspace_bytes", "lora_mixed_linear_backward_adapters", "retire_version_on",
-           "lml_multi_workspace_bytes", "lora_mixed_linear_multi")
+           "lml_multi_workspace_bytes", "lora_mixed_linear_multi", "lml_checkpoint_data_bytes", "lml_checkpoint_scale_bytes",
+           "lml_checkpoint_store", "lml_checkpoint_load", "lml_backward_rows_workspace_bytes",
+           "lora_mixed_linear_backward_adapters_rows", "lml_block_norm", "lml_block_norm_workspace_bytes",
+           "lml_block_norm_backward")
+ROWS_BF16, ROWS_INT8, ROWS_E4M3 = 0, 1, 2
+ROW_FORMS = {"bf16": ROWS_BF16, "int8": ROWS_INT8, "e4m3": ROWS_E4M3}
+MAX_NORM_WIDTH = 16384
+
+
+class Rows(ctypes.Structure):
+    """lml_rows: rows of activations, bf16 or an 8-bit checkpoint."""
+    _fields_ = [("data", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("format", ctypes.c_int)]
+
+
+class BlockNormDesc(ctypes.Structure):
+    """lml_block_norm_desc."""
+    _fields_ = [("d", ctypes.c_int), ("eps", ctypes.c_float), ("scale", ctypes.c_float), ("w_post", ctypes.c_void_p),
+                ("w_pre", ctypes.c_void_p), ("gate", ctypes.c_void_p)]
 
 
 class LmlError(RuntimeError):
@@ -89,6 +106,19 @@ def lib() -> ctypes.CDLL:
         L.lml_multi_workspace_bytes.argtypes = [ctypes.POINTER(vp), i32, i32]
         L.lora_mixed_linear_multi.argtypes = [ctypes.POINTER(vp), i32, vp, ctypes.POINTER(vp), i32, ctypes.POINTER(vp),
                                               ctypes.POINTER(vp), vp, sz, vp]
+        rows, desc = ctypes.POINTER(Rows), ctypes.POINTER(BlockNormDesc)
+        L.lml_checkpoint_data_bytes.argtypes = [i32, i32]
+        L.lml_checkpoint_scale_bytes.argtypes = [i32, i32]
+        L.lml_checkpoint_store.argtypes = [i32, vp, i32, i32, rows, vp]
+        L.lml_checkpoint_load.argtypes = [i32, rows, i32, i32, vp, vp]
+        L.lml_backward_rows_workspace_bytes.argtypes = [vp, i32, i32]
+        L.lora_mixed_linear_backward_adapters_rows.argtypes = [vp, vp, rows, vp, i32, vp, vp, vp, i32, vp, vp, i32, vp, sz, vp]
+        L.lml_block_norm.argtypes = [i32, desc, i32, vp, vp, vp, vp, vp, rows, rows, vp]
+        L.lml_block_norm_workspace_bytes.argtypes = [i32, i32, i32]
+        L.lml_block_norm_backward.argtypes = [i32, desc, i32, rows, rows, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        for name in ("lml_checkpoint_data_bytes", "lml_checkpoint_scale_bytes", "lml_backward_rows_workspace_bytes",
+                     "lml_block_norm_workspace_bytes"):
+            getattr(L, name).restype = sz
         L.lml_publish.argtypes = [vp, i32, i32, vp, ctypes.POINTER(i32)]
         L.lml_pin.argtypes = [vp, i32]
         L.lml_unpin.argtypes = [vp, i32]
@@ -99,7 +129,8 @@ def lib() -> ctypes.CDLL:
         for name in EXPORTS:
             if name not in ("lml_status_string", "lml_workspace_bytes", "lml_host_workspace_bytes",
                             "lml_tokens_workspace_bytes", "lml_dual_workspace_bytes", "lml_backward_workspace_bytes",
-                            "lml_multi_workspace_bytes"):
+                            "lml_multi_workspace_bytes", "lml_checkpoint_data_bytes", "lml_checkpoint_scale_bytes",
+                            "lml_backward_rows_workspace_bytes", "lml_block_norm_workspace_bytes"):
                 getattr(L, name).restype = i32
         _lib = L
     return _lib
@@ -306,6 +337,52 @@ def lora_mixed_linear_decode_static(table: int, x_ptr: int, W0_ptr: int, T: int,
                                                  perm_ptr, y_ptr, stream), "lora_mixed_linear_decode_static")
 
 
+def lml_checkpoint_data_bytes(T: int, d: int) -> int:
+    return int(lib().lml_checkpoint_data_bytes(T, d))
+
+
+def lml_checkpoint_scale_bytes(T: int, d: int) -> int:
+    return int(lib().lml_checkpoint_scale_bytes(T, d))
+
+
+def lml_checkpoint_store(device: int, x_ptr: int, T: int, d: int, kept: Rows, stream: int = 0) -> None:
+    _check(lib().lml_checkpoint_store(device, x_ptr, T, d, kept, stream), "lml_checkpoint_store")
+
+
+def lml_checkpoint_load(device: int, kept: Rows, T: int, d: int, x_ptr: int, stream: int = 0) -> None:
+    _check(lib().lml_checkpoint_load(device, kept, T, d, x_ptr, stream), "lml_checkpoint_load")
+
+
+def lml_backward_rows_workspace_bytes(table: int, max_tokens: int, max_segments: int) -> int:
+    return int(lib().lml_backward_rows_workspace_bytes(table, max_tokens, max_segments))
+
+
+def lora_mixed_linear_backward_adapters_rows(table: int, table_T: int, x: Rows, dy_ptr: int, T: int, seg_offsets_ptr: int,
+                                             slot_ids_ptr: int, slot_ids_T_ptr: int, G: int, dA_ptr: int, dB_ptr: int,
+                                             accumulate: bool, workspace_ptr: int, workspace_bytes: int, stream: int = 0) -> None:
+    """dA, dB of one batch with x as bf16 rows or as a checkpoint; accumulate: added to, else written."""
+    _check(lib().lora_mixed_linear_backward_adapters_rows(table, table_T, x, dy_ptr, T, seg_offsets_ptr, slot_ids_ptr, slot_ids_T_ptr,
+                                                          G, dA_ptr, dB_ptr, 1 if accumulate else 0, workspace_ptr, workspace_bytes,
+                                                          stream), "lora_mixed_linear_backward_adapters_rows")
+
+
+def lml_block_norm(device: int, desc: BlockNormDesc, T: int, h_ptr: int, o_ptr: int, gate_rows_ptr: int, h_new_ptr: int, x_ptr: int,
+                   x_kept: Optional[Rows], h_kept: Optional[Rows], stream: int = 0) -> None:
+    _check(lib().lml_block_norm(device, desc, T, h_ptr, o_ptr, gate_rows_ptr, h_new_ptr, x_ptr, x_kept, h_kept, stream), "lml_block_norm")
+
+
+def lml_block_norm_workspace_bytes(device: int, T: int, d: int) -> int:
+    return int(lib().lml_block_norm_workspace_bytes(device, T, d))
+
+
+def lml_block_norm_backward(device: int, desc: BlockNormDesc, T: int, h_new: Optional[Rows], o: Optional[Rows], gate_rows_ptr: int,
+                            dx_ptr: int, dh_new_ptr: int, dh_ptr: int, d_o_ptr: int, dw_pre_ptr: int, dw_post_ptr: int, dgate_ptr: int,
+                            dgate_rows_ptr: int, workspace_ptr: int, workspace_bytes: int, stream: int = 0) -> None:
+    _check(lib().lml_block_norm_backward(device, desc, T, h_new, o, gate_rows_ptr, dx_ptr, dh_new_ptr, dh_ptr, d_o_ptr, dw_pre_ptr,
+                                         dw_post_ptr, dgate_ptr, dgate_rows_ptr, workspace_ptr, workspace_bytes, stream),
+           "lml_block_norm_backward")
+
+
 def lml_device_status(table: int, stream: int = 0) -> int:
     f = ctypes.c_uint32(0)
     _check(lib().lml_device_status(table, ctypes.byref(f), stream), "lml_device_status")
@@ -340,6 +417,142 @@ def _stream(stream) -> int:
             device = torch.cuda.current_device
             _current_raw_stream = lambda: raw(device())  # noqa: E731
     return int(_current_raw_stream())
+
+
+def _stream_on(device, stream) -> int:
+    """The given stream, or the current one of the tensors' device (which need not be the current device)."""
+    if stream is not None:
+        return int(stream.cuda_stream)
+    import torch
+    if device.index == torch.cuda.current_device():
+        return _stream(None)
+    return int(torch.cuda.current_stream(device).cuda_stream)
+
+
+def _bf16_rows(t, T, d, name, device=None):
+    """Checks a bf16 [T][d] tensor of the call; None passes."""
+    import torch
+    if t is not None:
+        assert t.dtype == torch.bfloat16 and t.is_cuda and t.is_contiguous() and tuple(t.shape) == (T, d), (name, t.shape, t.dtype)
+        assert device is None or t.device == device, (name, t.device)
+    return t
+
+
+class Checkpoint:
+    """Activations kept in 8 bits (`form` "int8" or "e4m3") with a power-of-two scale per row and 32 columns; see lml_rows in the C header.
+    data uint8 [T][width up to a multiple of 32], scales uint8 [ceil(width / 128)][T][4]."""
+
+    def __init__(self, data, scales, width: int, form: str):
+        import torch
+        T = int(data.shape[0])
+        assert form in ("int8", "e4m3"), form
+        assert data.dtype == torch.uint8 and scales.dtype == torch.uint8 and data.is_cuda and scales.device == data.device
+        assert data.is_contiguous() and scales.is_contiguous() and width > 0 and width % 8 == 0
+        assert tuple(data.shape) == (T, (width + 31) // 32 * 32) and tuple(scales.shape) == ((width + 127) // 128, T, 4), (data.shape, scales.shape)
+        self.data, self.scales, self.tokens, self.width, self.form = data, scales, T, int(width), form
+        self.rows = Rows(_ptr(data), _ptr(scales), ROW_FORMS[form])
+
+    @classmethod
+    def empty(cls, tokens: int, width: int, form: str, device="cuda") -> "Checkpoint":
+        import torch
+        return cls(torch.empty((tokens, (width + 31) // 32 * 32), dtype=torch.uint8, device=device),
+                   torch.empty(((width + 127) // 128, tokens, 4), dtype=torch.uint8, device=device), width, form)
+
+    def nbytes(self) -> int:
+        return int(self.data.numel() + self.scales.numel())
+
+    def store(self, x, stream=None) -> "Checkpoint":
+        """Keep x (bf16 [tokens][width])."""
+        _bf16_rows(x, self.tokens, self.width, "x", self.data.device)
+        lml_checkpoint_store(x.device.index, _ptr(x), self.tokens, self.width, self.rows, _stream_on(x.device, stream))
+        return self
+
+    def load(self, out=None, stream=None):
+        """The values it stands for, bf16 [tokens][width]."""
+        import torch
+        dev = self.data.device
+        if out is None:
+            out = torch.empty((self.tokens, self.width), dtype=torch.bfloat16, device=dev)
+        _bf16_rows(out, self.tokens, self.width, "out", dev)
+        lml_checkpoint_load(dev.index, self.rows, self.tokens, self.width, _ptr(out), _stream_on(dev, stream))
+        return out
+
+
+def checkpoint_store(x, form: str = "int8", stream=None) -> Checkpoint:
+    """A new checkpoint of x (bf16 [T][d])."""
+    return Checkpoint.empty(int(x.shape[0]), int(x.shape[1]), form, x.device).store(x, stream)
+
+
+def _as_rows(x, T, d, name, device):
+    """Rows of a call: a bf16 tensor or a Checkpoint."""
+    if x is None:
+        return None
+    if isinstance(x, Checkpoint):
+        assert x.tokens == T and x.width == d and x.data.device == device, (name, x.tokens, x.width)
+        return x.rows
+    _bf16_rows(x, T, d, name, device)
+    return Rows(_ptr(x), None, ROWS_BF16)
+
+
+class BlockNorm:
+    """The norms between two blocks (lml_block_norm): weights and gate bf16 [d] or None, kept by the caller's program.
+
+        n = rmsnorm(o) w_post;  h' = h + scale gate n;  x = rmsnorm(h') w_pre
+    """
+
+    def __init__(self, d: int, w_post=None, w_pre=None, gate=None, scale: float = 1.0, eps: float = 1e-5):
+        import torch
+        for name, w in (("w_post", w_post), ("w_pre", w_pre), ("gate", gate)):
+            assert w is None or (w.dtype == torch.bfloat16 and w.is_cuda and w.is_contiguous() and tuple(w.shape) == (d,)), name
+        self.d, self.w_post, self.w_pre, self.gate, self.scale, self.eps = d, w_post, w_pre, gate, float(scale), float(eps)
+        self.device = next((w.device for w in (w_post, w_pre, gate) if w is not None), None)
+        self.desc = BlockNormDesc(d, eps, scale, _ptr(w_post), _ptr(w_pre), _ptr(gate))
+
+    def forward(self, h, o=None, gate_rows=None, h_new=None, x=None, x_checkpoint=None, h_checkpoint=None, stream=None):
+        """-> (h', x).  o None: h' is h.  gate_rows: a gate per token, bf16 [T][d].  h_new / x: where to write them (new tensors otherwise);
+        x_checkpoint / h_checkpoint: Checkpoints that the same pass fills.  x is None without w_pre."""
+        import torch
+        T, d, dev = int(h.shape[0]), self.d, h.device
+        assert self.device is None or dev == self.device, dev
+        for name, t in (("h", h), ("o", o), ("gate_rows", gate_rows), ("h_new", h_new), ("x", x)):
+            _bf16_rows(t, T, d, name, dev)
+        if h_new is None and o is not None:
+            h_new = torch.empty_like(h)
+        if x is None and self.w_pre is not None:
+            x = torch.empty_like(h)
+        lml_block_norm(dev.index, self.desc, T, _ptr(h), _ptr(o), _ptr(gate_rows), _ptr(h_new), _ptr(x),
+                       _as_rows(x_checkpoint, T, d, "x_checkpoint", dev), _as_rows(h_checkpoint, T, d, "h_checkpoint", dev),
+                       _stream_on(dev, stream))
+        return (h if o is None else h_new), x
+
+    def backward(self, h_new, o, dx, dh_new, gate_rows=None, dh=None, d_o=None, dw_pre=None, dw_post=None, dgate=None, workspace=None,
+                 stream=None):
+        """-> (dh, d_o, dgate).  h_new and o: bf16 tensors or Checkpoints; dx, dh_new: the gradients of x and h' (either may be None).
+        dw_pre, dw_post, dgate: float32 [d] that the sums over the tokens are added to, or None (frozen).  The third result is dgate, or with
+        gate_rows their gradient, bf16 [T][d]."""
+        import torch
+        some = dx if dx is not None else dh_new
+        T, d, dev = int(some.shape[0]), self.d, some.device
+        assert self.device is None or dev == self.device, dev
+        for name, t in (("dx", dx), ("dh_new", dh_new), ("gate_rows", gate_rows), ("dh", dh), ("d_o", d_o)):
+            _bf16_rows(t, T, d, name, dev)
+        for name, t in (("dw_pre", dw_pre), ("dw_post", dw_post), ("dgate", dgate)):
+            assert t is None or (t.dtype == torch.float32 and t.is_contiguous() and tuple(t.shape) == (d,) and t.device == dev), name
+        if dh is None:
+            dh = torch.empty_like(some)
+        if d_o is None and o is not None:
+            d_o = torch.empty_like(some)
+        dgate_rows = torch.empty_like(gate_rows) if gate_rows is not None else None
+        n_ws = 0
+        if dw_pre is not None or dw_post is not None or dgate is not None:
+            n_ws = lml_block_norm_workspace_bytes(dev.index, T, d)
+            if workspace is None:
+                workspace = torch.empty(max(n_ws, 256), dtype=torch.uint8, device=dev)
+            n_ws = int(workspace.numel())
+        lml_block_norm_backward(dev.index, self.desc, T, _as_rows(h_new, T, d, "h_new", dev), _as_rows(o, T, d, "o", dev), _ptr(gate_rows),
+                                _ptr(dx), _ptr(dh_new), _ptr(dh), _ptr(d_o), _ptr(dw_pre), _ptr(dw_post), _ptr(dgate), _ptr(dgate_rows),
+                                _ptr(workspace) if n_ws else 0, n_ws, _stream_on(dev, stream))
+        return dh, d_o, (dgate_rows if gate_rows is not None else dgate)
 
 
 def fuse_projection_adapters(parts):
@@ -501,6 +714,22 @@ class Table:
         lora_mixed_linear_backward_adapters(self.handle, table_T.handle, _ptr(x), _ptr(dy), T, _ptr(seg_offsets),
                                             _ptr(slot_ids), _ptr(slot_ids_T), G, _ptr(dA), _ptr(dB), _ptr(ws),
                                             int(ws.numel()), _stream(stream))
+
+    def backward_adapters_rows(self, table_T, x, dy, seg_offsets, slot_ids, slot_ids_T, dA, dB, accumulate=True, workspace=None, stream=None):
+        """backward_adapters with x as a Checkpoint (or a bf16 tensor) and unrounded small products.  accumulate=False: the rows j < rank of
+        every live slot are written, so that dA and dB need not be zeroed before a step's first batch."""
+        import torch
+        T, G, dev = int(dy.shape[0]), int(slot_ids.shape[0]), dy.device
+        assert dA.dtype == torch.float32 and dB.dtype == torch.float32 and dA.is_contiguous() and dB.is_contiguous()
+        assert tuple(dA.shape) == (self.max_slots, 64, self.d_in) and tuple(dB.shape) == (self.max_slots, self.d_out, 64)
+        assert seg_offsets.dtype == slot_ids.dtype == slot_ids_T.dtype == torch.int32
+        assert int(seg_offsets.shape[0]) == G + 1 and int(slot_ids_T.shape[0]) == G
+        _bf16_rows(dy, T, self.d_out, "dy")
+        if workspace is None:
+            workspace = torch.empty(max(lml_backward_rows_workspace_bytes(self.handle, T, G), 256), dtype=torch.uint8, device=dev)
+        lora_mixed_linear_backward_adapters_rows(self.handle, table_T.handle, _as_rows(x, T, self.d_in, "x", dev), _ptr(dy), T,
+                                                 _ptr(seg_offsets), _ptr(slot_ids), _ptr(slot_ids_T), G, _ptr(dA), _ptr(dB), accumulate,
+                                                 _ptr(workspace), int(workspace.numel()), _stream_on(dev, stream))
 
     def lora_mixed_linear_dual(self, x, W0, seg_offsets, slot_ids_a, slot_ids_b, perm=None, stream=None):
         """-> (y_a, y_b): the layer under two slot bindings of the same segments."""

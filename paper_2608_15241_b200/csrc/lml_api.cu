@@ -1,8 +1,10 @@
 // Host side of the C ABI: the adapter slot table, argument validation, workspace layout and
 // dispatch to the decode / prefill kernels.  See include/lora_mixed_linear.h for the contract.
+#include <atomic>
 #include <cstdlib>
 #include <new>
 
+#include "lml_rows_grad.cuh"
 #include "lml_table.cuh"
 
 using namespace lml;
@@ -252,6 +254,7 @@ lml_status lml_table_create(lml_table** out, int device, int d_in, int d_out, in
     ok = ok && shrink_init() == cudaSuccess;
     ok = ok && aux_init() == cudaSuccess;
     ok = ok && bind_init() == cudaSuccess;
+    ok = ok && rows_grad_init() == cudaSuccess;
     ok = ok && encode_tmap_3d(&t->tmap_A, t->arena.A, (uint64_t)d_in, kRankPad, (uint64_t)max_slots, (uint64_t)d_in * 2,
                               (uint64_t)d_in * kRankPad * 2, 64, kChunk, 1);
     gemm_split_override(&t->split_bn, &t->split_s);   // the test knobs are read here, never on the hot path
@@ -966,6 +969,162 @@ lml_status lora_mixed_linear_host(lml_table* t, const void* x_host, const void* 
         cudaGetLastError();
         return LML_ERR_CUDA;
     }
+    return LML_OK;
+}
+
+// ---- rows: checkpoints, gradients from them, block norms --------------------------------------------------
+
+static bool rows_ok(const lml_rows* r, bool bf16_too)
+{
+    if (!r || !r->data || !aligned16(r->data)) return false;
+    if (r->format == LML_ROWS_BF16) return bf16_too;
+    return (r->format == LML_ROWS_INT8 || r->format == LML_ROWS_E4M3) && r->scales && aligned16(r->scales);
+}
+static Rows as_rows(const lml_rows* r) { return r ? Rows{r->data, static_cast<uint32_t*>(r->scales), r->format} : Rows{nullptr, nullptr, LML_ROWS_BF16}; }
+static bool rows_sizes_ok(int T, int d) { return T >= 0 && T <= kMaxTokens && d > 0 && d % 8 == 0 && d <= (1 << 24); }
+
+size_t lml_checkpoint_data_bytes(int T, int d) { return rows_sizes_ok(T, d) ? (size_t)T * kept_pitch(d) : 0; }
+size_t lml_checkpoint_scale_bytes(int T, int d) { return rows_sizes_ok(T, d) ? (size_t)T * kept_groups(d) * 4 : 0; }
+
+lml_status lml_checkpoint_store(int device, const void* x, int T, int d, const lml_rows* kept, void* stream)
+{
+    if (device < 0 || !rows_sizes_ok(T, d)) return LML_ERR_INVALID_ARG;
+    if (T == 0) return LML_OK;
+    if (!x || !aligned16(x) || !rows_ok(kept, false)) return LML_ERR_INVALID_ARG;
+    DeviceGuard guard(device);
+    if (!guard.ok) { cudaGetLastError(); return LML_ERR_CUDA; }
+    if (launch_kept_store(x, T, d, as_rows(kept), (cudaStream_t)stream) != cudaSuccess) { cudaGetLastError(); return LML_ERR_CUDA; }
+    return LML_OK;
+}
+
+lml_status lml_checkpoint_load(int device, const lml_rows* kept, int T, int d, void* x, void* stream)
+{
+    if (device < 0 || !rows_sizes_ok(T, d)) return LML_ERR_INVALID_ARG;
+    if (T == 0) return LML_OK;
+    if (!x || !aligned16(x) || !rows_ok(kept, false)) return LML_ERR_INVALID_ARG;
+    DeviceGuard guard(device);
+    if (!guard.ok) { cudaGetLastError(); return LML_ERR_CUDA; }
+    if (launch_kept_load(as_rows(kept), T, d, x, (cudaStream_t)stream) != cudaSuccess) { cudaGetLastError(); return LML_ERR_CUDA; }
+    return LML_OK;
+}
+
+size_t lml_backward_rows_workspace_bytes(const lml_table* t, int max_tokens, int max_segments)
+{
+    if (!t || max_tokens < 0 || max_segments < 0 || max_tokens > kMaxTokens || max_segments > kMaxTokens) return 0;
+    return rows_grad_ws_bytes(max_tokens, max_segments > 0 ? max_segments : 1);
+}
+
+lml_status lora_mixed_linear_backward_adapters_rows(lml_table* t, lml_table* t_T, const lml_rows* x, const void* dy, int T,
+                                                    const int32_t* seg_offsets, const int32_t* slot_ids,
+                                                    const int32_t* slot_ids_T, int G, float* dA, float* dB, int accumulate,
+                                                    void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!t || !t_T || T < 0 || G < 1 || T > kMaxTokens || G > kMaxTokens) return LML_ERR_INVALID_ARG;
+    if (t_T->d_in != t->d_out || t_T->d_out != t->d_in || t_T->device != t->device) return LML_ERR_INVALID_ARG;
+    if (T == 0 && accumulate) { t->last_launches = 0; return LML_OK; }
+    if (!dA || !dB || !aligned16(dA) || !aligned16(dB)) return LML_ERR_INVALID_ARG;
+    if (T > 0) {
+        if (!dy || !aligned16(dy) || !rows_ok(x, true) || !seg_offsets || !slot_ids || !slot_ids_T) return LML_ERR_INVALID_ARG;
+        if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < rows_grad_ws_bytes(T, G)) return LML_ERR_WORKSPACE;
+    }
+    const SlotSnapshot snap = snapshot_locked(t);
+    const SlotSnapshot snap_T = snapshot_locked(t_T);
+    DeviceGuard guard(t->device);
+    if (!guard.ok) return LML_ERR_CUDA;
+    RowsGradCall a;
+    a.snap = &snap; a.snap_T = &snap_T;
+    a.tmap_A = &t->tmap_A; a.tmap_AT = &t_T->tmap_A;
+    a.cache = &t->tmaps;
+    a.status = t->arena.status; a.status_T = t_T->arena.status;
+    a.x = T > 0 ? as_rows(x) : Rows{nullptr, nullptr, LML_ROWS_BF16};
+    a.dy = dy;
+    a.seg_offsets = seg_offsets; a.ids = slot_ids; a.ids_T = slot_ids_T;
+    a.dA = dA; a.dB = dB;
+    a.workspace = workspace;
+    a.T = T; a.G = G; a.d_in = t->d_in; a.d_out = t->d_out; a.num_sms = t->num_sms;
+    a.accumulate = accumulate != 0;
+    int launches = 0;
+    const cudaError_t e = launch_rows_grad(a, (cudaStream_t)stream, &launches);
+    t->last_launches = launches;
+    if (e != cudaSuccess) { cudaGetLastError(); return LML_ERR_CUDA; }
+    return LML_OK;
+}
+
+// Multiprocessors of a device, asked once; 0: no such device.
+static int sms_of(int device)
+{
+    static std::atomic<int> known[64];
+    if (device < 0) return 0;
+    int n = device < 64 ? known[device].load(std::memory_order_relaxed) : 0;
+    if (n == 0) {
+        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) { cudaGetLastError(); return 0; }
+        if (device < 64) known[device].store(n, std::memory_order_relaxed);
+    }
+    return n;
+}
+
+static bool norm_desc_ok(int device, const lml_block_norm_desc* p, int T)
+{
+    if (device < 0 || !p || T < 0 || T > kMaxTokens || p->d <= 0 || p->d % 8 || p->d > LML_MAX_NORM_WIDTH) return false;
+    if (!(p->eps > 0.f) || !(p->scale == p->scale)) return false;
+    return aligned16(p->w_post) && aligned16(p->w_pre) && aligned16(p->gate);
+}
+static NormArgs norm_args(const lml_block_norm_desc* p, int T, const void* gate_rows)
+{
+    return NormArgs{T, p->d, p->eps, p->scale, p->w_post, p->w_pre, p->gate, gate_rows};
+}
+
+lml_status lml_block_norm(int device, const lml_block_norm_desc* desc, int T, const void* h, const void* o, const void* gate_rows,
+                          void* h_new, void* x, const lml_rows* x_kept, const lml_rows* h_kept, void* stream)
+{
+    if (!norm_desc_ok(device, desc, T)) return LML_ERR_INVALID_ARG;
+    if (T == 0) return LML_OK;
+    if (!h || !aligned16(h) || !aligned16(o) || !aligned16(gate_rows) || !aligned16(h_new) || !aligned16(x)) return LML_ERR_INVALID_ARG;
+    if ((x_kept && !rows_ok(x_kept, false)) || (h_kept && !rows_ok(h_kept, false))) return LML_ERR_INVALID_ARG;
+    if (!o && (h_new || gate_rows)) return LML_ERR_INVALID_ARG;
+    if (gate_rows && desc->gate) return LML_ERR_INVALID_ARG;
+    if (!desc->w_pre && (x || x_kept)) return LML_ERR_INVALID_ARG;
+    if (!h_new && !x && !x_kept && !h_kept) return LML_ERR_INVALID_ARG;
+    const int sms = sms_of(device);
+    DeviceGuard guard(device);
+    if (!guard.ok || sms == 0) { cudaGetLastError(); return LML_ERR_CUDA; }
+    NormForward a{norm_args(desc, T, gate_rows), h, o, h_new, x, as_rows(x_kept), as_rows(h_kept)};
+    if (!x && !x_kept) a.n.w_pre = nullptr;
+    if (launch_block_norm(a, sms, (cudaStream_t)stream) != cudaSuccess) { cudaGetLastError(); return LML_ERR_CUDA; }
+    return LML_OK;
+}
+
+size_t lml_block_norm_workspace_bytes(int device, int T, int d)
+{
+    if (!rows_sizes_ok(T, d) || d > LML_MAX_NORM_WIDTH) return 0;
+    const int sms = sms_of(device);
+    return sms ? norm_backward_ws_bytes(T, d, sms) : 0;
+}
+
+lml_status lml_block_norm_backward(int device, const lml_block_norm_desc* desc, int T, const lml_rows* h_new, const lml_rows* o,
+                                   const void* gate_rows, const void* dx, const void* dh_new, void* dh, void* d_o, float* dw_pre,
+                                   float* dw_post, float* dgate, void* dgate_rows, void* workspace, size_t workspace_bytes,
+                                   void* stream)
+{
+    if (!norm_desc_ok(device, desc, T)) return LML_ERR_INVALID_ARG;
+    if (T == 0) return LML_OK;
+    if ((!dx && !dh_new) || (dx && (!desc->w_pre || !rows_ok(h_new, true))) || (o && !rows_ok(o, true))) return LML_ERR_INVALID_ARG;
+    if (!aligned16(gate_rows) || !aligned16(dx) || !aligned16(dh_new) || !aligned16(dh) || !aligned16(d_o) || !aligned16(dw_pre) ||
+        !aligned16(dw_post) || !aligned16(dgate) || !aligned16(dgate_rows))
+        return LML_ERR_INVALID_ARG;
+    if ((gate_rows && desc->gate) || (dw_pre && !dx) || (!o && (d_o || dw_post || dgate || dgate_rows || gate_rows))) return LML_ERR_INVALID_ARG;
+    if ((dw_post && !desc->w_post) || (dgate && !desc->gate) || (dgate_rows && !gate_rows)) return LML_ERR_INVALID_ARG;
+    if (!dh && !d_o && !dw_pre && !dw_post && !dgate && !dgate_rows) return LML_ERR_INVALID_ARG;
+    const int sms = sms_of(device);
+    if (sms == 0) return LML_ERR_CUDA;
+    if ((dw_pre || dw_post || dgate) && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) ||
+                                         workspace_bytes < norm_backward_ws_bytes(T, desc->d, sms)))
+        return LML_ERR_WORKSPACE;
+    DeviceGuard guard(device);
+    if (!guard.ok) { cudaGetLastError(); return LML_ERR_CUDA; }
+    const NormBackward a{norm_args(desc, T, gate_rows), dx ? as_rows(h_new) : as_rows(nullptr), as_rows(o), dx, dh_new, dh, d_o, dgate_rows,
+                         dw_pre, dw_post, dgate, static_cast<float*>(workspace)};
+    if (launch_block_norm_backward(a, sms, (cudaStream_t)stream) != cudaSuccess) { cudaGetLastError(); return LML_ERR_CUDA; }
     return LML_OK;
 }
 

@@ -1,0 +1,186 @@
+// Rows of activations as the training calls take them: bf16, or an 8-bit checkpoint.
+//
+// A checkpoint holds, per row and 32 columns, 8-bit values q and one power of two 2^(b - 127) (the OCP Microscaling
+// formats MXINT8, its steps counted as integers, and MXFP8 E4M3); a value is q * 2^(b - 127).  Powers of two, because a
+// decoded value then is exact in bf16 (q has at most 7 significant bits): what the tensor cores multiply is what the
+// checkpoint stands for, and the only rounding of the whole path is that of q, half a step at most.
+//   int8: b = E + 121 with E the binade of the block's largest value, |q| <= 127: the largest bf16 value of a binade is
+//         127.5 steps, so the clamp is half a step as well.
+//   e4m3: the least b with amax <= 448 * 2^(b - 127).  (Values of 1.9375 * 2^127 and more, 3.3e38, become 1.875 * 2^127.)
+// b = 0 (2^-127) at least, 3 for e4m3 (its smallest step is then 2^-133, bf16's); a block that holds Inf or NaN has
+// b = 255 and reads back as NaN throughout.
+//
+// Layout: q [T][pitch], pitch = d up to a multiple of 32, zeros behind column d; b in words of four blocks (128 columns),
+// [column group][T]: a tile of 128 columns reads its scales as one contiguous piece, a row writes one word per 128 columns.
+#pragma once
+#include <cuda_fp8.h>
+
+#include "lml_internal.cuh"
+
+namespace lml {
+
+enum RowFormat { kBf16 = LML_ROWS_BF16, kInt8 = LML_ROWS_INT8, kE4m3 = LML_ROWS_E4M3 };
+
+__host__ __device__ __forceinline__ int kept_pitch(int d) { return (d + 31) / 32 * 32; }
+__host__ __device__ __forceinline__ int kept_groups(int d) { return (d + 127) / 128; }
+
+// Rows as a kernel reads or writes them.
+struct Rows {
+    void* data;
+    uint32_t* scales;   // word [column group][T]
+    int format;
+};
+
+// 2^(b - 127); NaN for b = 255
+__device__ __forceinline__ float scale_of_byte(uint32_t b)
+{
+    return __uint_as_float(b == 0 ? 0x00400000u : b == 255u ? 0x7fc00000u : b << 23);
+}
+// scale byte of a block from the largest |value| of it, as the bits of a bf16
+__device__ __forceinline__ uint32_t byte_of_amax(uint32_t amax, bool e4m3)
+{
+    const uint32_t ef = amax >> 7, mant = amax & 0x7fu;
+    if (ef == 255u) return 255u;
+    const int b = e4m3 ? (int)ef - 8 + (mant > 0x60u ? 1 : 0) : (int)ef - 6;
+    return (uint32_t)max(b, e4m3 ? 3 : 0);
+}
+
+// The scale byte of e4m3 blocks whose largest value is beyond 1.75 * 2^127: 248 units and more would round to 2^128, which bf16 does not
+// have, so they become 240 units (1.875 * 2^127).
+constexpr uint32_t kTopByte = 247u;
+
+// Eight consecutive values, packed bf16 -> 8 bits; byte: their block's scale byte.
+__device__ __forceinline__ uint2 encode8(const uint4& v, uint32_t byte, bool e4m3)
+{
+    const float inv = byte == 255u ? 0.f : __uint_as_float((254u - byte) << 23);   // 2^(127 - byte)
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t out[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        float a = bf16_lo(w[2 * h]) * inv, b = bf16_hi(w[2 * h]) * inv, c = bf16_lo(w[2 * h + 1]) * inv, d = bf16_hi(w[2 * h + 1]) * inv;
+        if (e4m3) {
+            if (byte == kTopByte) {
+                a = fminf(fmaxf(a, -240.f), 240.f); b = fminf(fmaxf(b, -240.f), 240.f);
+                c = fminf(fmaxf(c, -240.f), 240.f); d = fminf(fmaxf(d, -240.f), 240.f);
+            }
+            const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+            const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
+            out[h] = lo | hi << 16;
+        } else {
+            // rounding to an integer by adding 1.5 * 2^23: the low byte of the sum's bits is q in two's complement
+            const float m = 12582912.f;
+            const uint32_t qa = __float_as_uint(fminf(fmaxf(a, -127.f), 127.f) + m), qb = __float_as_uint(fminf(fmaxf(b, -127.f), 127.f) + m);
+            const uint32_t qc = __float_as_uint(fminf(fmaxf(c, -127.f), 127.f) + m), qd = __float_as_uint(fminf(fmaxf(d, -127.f), 127.f) + m);
+            out[h] = __byte_perm(__byte_perm(qa, qb, 0x0040), __byte_perm(qc, qd, 0x0040), 0x5410);
+        }
+    }
+    return make_uint2(out[0], out[1]);
+}
+// Four 8-bit values -> fp32, times their block's scale (exact).
+__device__ __forceinline__ void decode4(uint32_t q, float s, bool e4m3, float& a, float& b, float& c, float& d)
+{
+    if (e4m3) {
+        const __half2 lo(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(q & 0xffffu), __NV_E4M3));
+        const __half2 hi(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(q >> 16), __NV_E4M3));
+        const float2 l = __half22float2(lo), h = __half22float2(hi);
+        a = l.x * s; b = l.y * s; c = h.x * s; d = h.y * s;
+    } else {
+        // 0x4b0000uu is 2^23 + uu; uu = q + 128
+        const uint32_t u = q ^ 0x80808080u;
+        const float bias = 8388736.f;
+        a = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440)) - bias) * s;
+        b = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7441)) - bias) * s;
+        c = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7442)) - bias) * s;
+        d = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7443)) - bias) * s;
+    }
+}
+__device__ __forceinline__ uint4 decode8_bf16(const uint2& q, float s, bool e4m3)
+{
+    float f[8];
+    decode4(q.x, s, e4m3, f[0], f[1], f[2], f[3]);
+    decode4(q.y, s, e4m3, f[4], f[5], f[6], f[7]);
+    return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+}
+
+__device__ __forceinline__ uint32_t amax_bits(const uint4& v)   // largest |value| of eight, as bf16 bits
+{
+    const uint32_t m = 0x7fff7fffu;
+    const uint32_t a = __vmaxu2(__vmaxu2(v.x & m, v.y & m), __vmaxu2(v.z & m, v.w & m));
+    return max(a & 0xffffu, a >> 16);
+}
+
+// Vector `vec` (columns 8 vec ...) of row t of a checkpoint, by the 32 lanes of a converged warp that hold consecutive
+// vectors, the first a multiple of 32.  Lanes behind the last column pass zeros.
+__device__ __forceinline__ void store_kept(const Rows& r, int T, int d, long long t, int vec, const uint4& v)
+{
+    uint32_t amax = amax_bits(v);
+    amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+    amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+    const bool e4m3 = r.format == kE4m3;
+    const int pitch = kept_pitch(d);
+    const uint32_t byte = byte_of_amax(amax, e4m3);
+    if (vec * 8 < pitch) *reinterpret_cast<uint2*>(static_cast<uint8_t*>(r.data) + t * pitch + vec * 8) =
+            encode8(v, byte, e4m3);
+    uint32_t word = vec * 8 < pitch ? byte << (8 * ((vec >> 2) & 3)) : 0u;   // (blocks behind the last have scale byte 0)
+    word |= __shfl_xor_sync(0xffffffffu, word, 4);
+    word |= __shfl_xor_sync(0xffffffffu, word, 8);
+    if ((vec & 15) == 0 && vec * 8 < pitch) r.scales[(long long)(vec >> 4) * T + t] = word;
+}
+// Ordinary loads, not through the non-coherent path: the kernels start while the work that writes their inputs still runs, and
+// an output may be the buffer of an input.
+__device__ __forceinline__ uint4 ld_v4(const void* p)
+{
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint2 ld_v2(const void* p)
+{
+    uint2 v;
+    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint4 ld_weights(const void* p, int vec)   // (kept in L1: read for every row)
+{
+    uint4 v;
+    asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(static_cast<const uint4*>(p) + vec) : "memory");
+    return v;
+}
+// The vector as packed bf16; vec within the row.
+__device__ __forceinline__ uint4 load_rows(const Rows& r, int T, int d, long long t, int vec)
+{
+    if (r.format == kBf16) return ld_v4(static_cast<const __nv_bfloat16*>(r.data) + t * d + vec * 8);
+    const uint2 q = ld_v2(static_cast<const uint8_t*>(r.data) + t * kept_pitch(d) + vec * 8);
+    const uint32_t word = ld_after_wait(r.scales + (long long)(vec >> 4) * T + t);
+    return decode8_bf16(q, scale_of_byte((word >> (8 * ((vec >> 2) & 3))) & 0xffu), r.format == kE4m3);
+}
+
+// ---- launchers ------------------------------------------------------------------------------------
+cudaError_t launch_kept_store(const void* x, int T, int d, const Rows& out, cudaStream_t stream);
+cudaError_t launch_kept_load(const Rows& in, int T, int d, void* x, cudaStream_t stream);
+
+constexpr int kMaxNormWidth = LML_MAX_NORM_WIDTH;
+struct NormArgs {
+    int T, d;
+    float eps, scale;
+    const void *w_post, *w_pre, *gate, *gate_rows;
+};
+struct NormForward {
+    NormArgs n;
+    const void *h, *o;
+    void *h_new, *x;
+    Rows x_kept, h_kept;   // data null: not wanted
+};
+struct NormBackward {
+    NormArgs n;
+    Rows h_new, o;         // data null: not there
+    const void *dx, *dh_new;
+    void *dh, *d_o, *dgate_rows;
+    float *dw_pre, *dw_post, *dgate;
+    float* partial;        // workspace
+};
+cudaError_t launch_block_norm(const NormForward& a, int num_sms, cudaStream_t stream);
+cudaError_t launch_block_norm_backward(const NormBackward& a, int num_sms, cudaStream_t stream);
+size_t norm_backward_ws_bytes(int T, int d, int num_sms);
+
+}  // namespace lml

@@ -1,0 +1,24 @@
+// Adapter gradients with x as bf16 rows or as a checkpoint: what the host side of the library calls.
+#pragma once
+#include "lml_rows.cuh"
+
+namespace lml {
+
+struct RowsGradCall {
+    const SlotSnapshot *snap, *snap_T;
+    const CUtensorMap *tmap_A, *tmap_AT;   // the packed A of the table and of the transposed one
+    TmapCache* cache;
+    uint32_t *status, *status_T;
+    Rows x;
+    const void* dy;
+    const int32_t *seg_offsets, *ids, *ids_T;
+    float *dA, *dB;
+    void* workspace;
+    int T, G, d_in, d_out, num_sms;
+    bool accumulate;
+};
+size_t rows_grad_ws_bytes(int T, int G);
+cudaError_t rows_grad_init();   // sets the dynamic shared memory attributes
+cudaError_t launch_rows_grad(const RowsGradCall& a, cudaStream_t stream, int* launches);
+
+}  // namespace lml
