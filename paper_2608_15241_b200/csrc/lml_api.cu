@@ -171,7 +171,7 @@ cudaError_t run_gemm_path(const GemmCall* calls, int P, const void* x, int T, Ro
 
 static void free_table_resources(lml_table* t)
 {
-    cudaFree(t->arena.A); cudaFree(t->arena.B); cudaFree(t->arena.Bc); cudaFree(t->arena.Bk); cudaFree(t->arena.status); cudaFree(t->arena.adapter_map); cudaFree(t->arena.pass_flags); cudaFree(t->arena.dec_u);
+    cudaFree(t->arena.A); cudaFree(t->arena.B); cudaFree(t->arena.Bc); cudaFree(t->arena.Bk); cudaFree(t->arena.status); cudaFree(t->arena.adapter_map); cudaFree(t->arena.pass_flags); cudaFree(t->arena.dec_u); cudaFree(t->arena.rows_arrived);
     if (t->copy_in) cudaStreamDestroy(t->copy_in);
     if (t->copy_out) cudaStreamDestroy(t->copy_out);
     if (t->ev_begin) cudaEventDestroy(t->ev_begin);
@@ -248,6 +248,9 @@ lml_status lml_table_create(lml_table** out, int device, int d_in, int d_out, in
     ok = ok && cudaMemset(t->arena.adapter_map, 0xff, kMaxAdapterIds * sizeof(int32_t)) == cudaSuccess;   // -1: no serving version
     ok = ok && cudaMalloc(&t->arena.pass_flags, kFuseMaxPasses * sizeof(int32_t)) == cudaSuccess;
     ok = ok && cudaMemset(t->arena.pass_flags, 0, kFuseMaxPasses * sizeof(int32_t)) == cudaSuccess;
+    const size_t arrived_bytes = (size_t)t->num_sms * sizeof(int32_t);
+    ok = ok && cudaMalloc(&t->arena.rows_arrived, arrived_bytes) == cudaSuccess;
+    ok = ok && cudaMemset(t->arena.rows_arrived, 0, arrived_bytes) == cudaSuccess;
     ok = ok && decode_init() == cudaSuccess;   // (first: see there)
     ok = ok && gemm_sm100_init(device) == cudaSuccess;
     ok = ok && gemm_pair_init(t->num_sms, &t->num_pairs) == cudaSuccess;
@@ -1011,7 +1014,7 @@ lml_status lml_checkpoint_load(int device, const lml_rows* kept, int T, int d, v
 size_t lml_backward_rows_workspace_bytes(const lml_table* t, int max_tokens, int max_segments)
 {
     if (!t || max_tokens < 0 || max_segments < 0 || max_tokens > kMaxTokens || max_segments > kMaxTokens) return 0;
-    return rows_grad_ws_bytes(max_tokens, max_segments > 0 ? max_segments : 1);
+    return rows_grad_ws_bytes(max_tokens, max_segments > 0 ? max_segments : 1, t->num_sms);
 }
 
 lml_status lora_mixed_linear_backward_adapters_rows(lml_table* t, lml_table* t_T, const lml_rows* x, const void* dy, int T,
@@ -1025,7 +1028,8 @@ lml_status lora_mixed_linear_backward_adapters_rows(lml_table* t, lml_table* t_T
     if (!dA || !dB || !aligned16(dA) || !aligned16(dB)) return LML_ERR_INVALID_ARG;
     if (T > 0) {
         if (!dy || !aligned16(dy) || !rows_ok(x, true) || !seg_offsets || !slot_ids || !slot_ids_T) return LML_ERR_INVALID_ARG;
-        if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < rows_grad_ws_bytes(T, G)) return LML_ERR_WORKSPACE;
+        if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < rows_grad_ws_bytes(T, G, t->num_sms))
+            return LML_ERR_WORKSPACE;
     }
     const SlotSnapshot snap = snapshot_locked(t);
     const SlotSnapshot snap_T = snapshot_locked(t_T);
@@ -1033,7 +1037,8 @@ lml_status lora_mixed_linear_backward_adapters_rows(lml_table* t, lml_table* t_T
     if (!guard.ok) return LML_ERR_CUDA;
     RowsGradCall a;
     a.snap = &snap; a.snap_T = &snap_T;
-    a.tmap_A = &t->tmap_A; a.tmap_AT = &t_T->tmap_A;
+    a.low[0] = t->arena.A; a.low[1] = t_T->arena.A;
+    a.slots[0] = t->max_slots; a.slots[1] = t_T->max_slots;
     a.cache = &t->tmaps;
     a.status = t->arena.status; a.status_T = t_T->arena.status;
     a.x = T > 0 ? as_rows(x) : Rows{nullptr, nullptr, LML_ROWS_BF16};
@@ -1041,6 +1046,7 @@ lml_status lora_mixed_linear_backward_adapters_rows(lml_table* t, lml_table* t_T
     a.seg_offsets = seg_offsets; a.ids = slot_ids; a.ids_T = slot_ids_T;
     a.dA = dA; a.dB = dB;
     a.workspace = workspace;
+    a.arrived = t->arena.rows_arrived;
     a.T = T; a.G = G; a.d_in = t->d_in; a.d_out = t->d_out; a.num_sms = t->num_sms;
     a.accumulate = accumulate != 0;
     int launches = 0;
@@ -1142,6 +1148,7 @@ lml_status lml_device_status(lml_table* t, uint32_t* flags_out, void* stream_v)
         // a launch gave up on a wait: its counters may have been left behind, so the decode kernel's exchange blocks
         // start over (only then: in normal operation nothing here touches memory that a call in flight uses)
         ok = cudaMemsetAsync(t->arena.status + 8, 0, 2 * sizeof(uint32_t), stream) == cudaSuccess;
+        ok = ok && cudaMemsetAsync(t->arena.rows_arrived, 0, (size_t)t->num_sms * sizeof(int32_t), stream) == cudaSuccess;
         ok = ok && cudaMemsetAsync(t->arena.dec_u, 0, (size_t)kDecMaxBlocks * kDecExchStride * sizeof(unsigned long long), stream) == cudaSuccess;
         ok = ok && cudaStreamSynchronize(stream) == cudaSuccess;
     }

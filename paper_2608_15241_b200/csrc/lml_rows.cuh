@@ -31,11 +31,6 @@ struct Rows {
     int format;
 };
 
-// 2^(b - 127); NaN for b = 255
-__device__ __forceinline__ float scale_of_byte(uint32_t b)
-{
-    return __uint_as_float(b == 0 ? 0x00400000u : b == 255u ? 0x7fc00000u : b << 23);
-}
 // scale byte of a block from the largest |value| of it, as the bits of a bf16
 __device__ __forceinline__ uint32_t byte_of_amax(uint32_t amax, bool e4m3)
 {
@@ -76,30 +71,47 @@ __device__ __forceinline__ uint2 encode8(const uint4& v, uint32_t byte, bool e4m
     }
     return make_uint2(out[0], out[1]);
 }
-// Four 8-bit values -> fp32, times their block's scale (exact).
-__device__ __forceinline__ void decode4(uint32_t q, float s, bool e4m3, float& a, float& b, float& c, float& d)
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
 {
-    if (e4m3) {
-        const __half2 lo(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(q & 0xffffu), __NV_E4M3));
-        const __half2 hi(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(q >> 16), __NV_E4M3));
-        const float2 l = __half22float2(lo), h = __half22float2(hi);
-        a = l.x * s; b = l.y * s; c = h.x * s; d = h.y * s;
-    } else {
-        // 0x4b0000uu is 2^23 + uu; uu = q + 128
-        const uint32_t u = q ^ 0x80808080u;
-        const float bias = 8388736.f;
-        a = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440)) - bias) * s;
-        b = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7441)) - bias) * s;
-        c = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7442)) - bias) * s;
-        d = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7443)) - bias) * s;
-    }
+    uint32_t d;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
 }
-__device__ __forceinline__ uint4 decode8_bf16(const uint2& q, float s, bool e4m3)
+__device__ __forceinline__ uint32_t sub_bf16x2(uint32_t a, uint32_t b)
 {
-    float f[8];
-    decode4(q.x, s, e4m3, f[0], f[1], f[2], f[3]);
-    decode4(q.y, s, e4m3, f[4], f[5], f[6], f[7]);
-    return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+    uint32_t d;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+// Decoding, two values at a time, in integer and packed bf16 arithmetic, exact in every step.  What a block's scale byte b becomes for it:
+//   int8: 2^(b - 120), which is 128 units.  With q's low seven bits as mantissa it is 128 + q units, or 256 + q where q is negative; 128 or, one
+//         binade up, 256 units are taken off again.
+//   e4m3: sign, exponent and mantissa put in their places in bf16 are the value times 2^-120; the factor is 2^(b - 7).
+// Factors beyond the format (and NaN, b = 255) are the rare case: the value is made at scale 1 and multiplied.
+// (us for 8 KB by 256 threads: 0.21, and 0.34 with a subtraction and a multiplication each, 0.48 through fp32.)
+template <bool E4M3> struct Decoder {
+    uint32_t base;
+    static constexpr uint32_t kMost = E4M3 ? 134u : 246u;   // scale bytes of the usual case
+    __device__ __forceinline__ explicit Decoder(uint32_t b) : base((b + (E4M3 ? 120u : 7u)) * 0x00800080u) {}
+    __device__ __forceinline__ uint32_t pair(uint32_t q, int i) const   // bytes 2 i and 2 i + 1
+    {
+        if (E4M3) {
+            const uint32_t w = __byte_perm(q, 0u, i ? 0x3424 : 0x1404);
+            return mul_bf16x2((w & 0x80008000u) | ((w >> 4) & 0x07f007f0u), base);
+        }
+        const uint32_t w = __byte_perm(q, 0u, i ? 0x4342 : 0x4140);
+        return sub_bf16x2((w & 0x007f007fu) | base, (w & 0x00800080u) + base);
+    }
+    __device__ __forceinline__ uint4 eight(const uint2& q) const { return make_uint4(pair(q.x, 0), pair(q.x, 1), pair(q.y, 0), pair(q.y, 1)); }
+};
+// ... of a block with any scale byte
+template <bool E4M3>
+__device__ __forceinline__ uint4 decode8(const uint2& q, uint32_t b)
+{
+    if (b <= Decoder<E4M3>::kMost) return Decoder<E4M3>(b).eight(q);
+    const uint4 v = Decoder<E4M3>(127u).eight(q);
+    const uint32_t s = (b == 255u ? 0x7fc0u : b << 7) * 0x10001u;
+    return make_uint4(mul_bf16x2(v.x, s), mul_bf16x2(v.y, s), mul_bf16x2(v.z, s), mul_bf16x2(v.w, s));
 }
 
 __device__ __forceinline__ uint32_t amax_bits(const uint4& v)   // largest |value| of eight, as bf16 bits
@@ -152,7 +164,8 @@ __device__ __forceinline__ uint4 load_rows(const Rows& r, int T, int d, long lon
     if (r.format == kBf16) return ld_v4(static_cast<const __nv_bfloat16*>(r.data) + t * d + vec * 8);
     const uint2 q = ld_v2(static_cast<const uint8_t*>(r.data) + t * kept_pitch(d) + vec * 8);
     const uint32_t word = ld_after_wait(r.scales + (long long)(vec >> 4) * T + t);
-    return decode8_bf16(q, scale_of_byte((word >> (8 * ((vec >> 2) & 3))) & 0xffu), r.format == kE4m3);
+    const uint32_t byte = (word >> (8 * ((vec >> 2) & 3))) & 0xffu;
+    return r.format == kE4m3 ? decode8<true>(q, byte) : decode8<false>(q, byte);
 }
 
 // ---- launchers ------------------------------------------------------------------------------------

@@ -2,19 +2,24 @@
 //     u = s x.A^T,  v = s dy.B   (per token, with the token's adapter)        dA_s += v^T x,   dB_s += dy^T u
 // Two launches, each over x and dy side by side.
 //
-// rows_shrink_kernel: u and v.  A piece is up to 128 rows of one segment, counted from the segment's first row (a TMA box may
-// begin at any row), so no row of another segment is in it but behind its end.  A cluster of S CTAs shares the columns; partial
-// products meet through distributed shared memory in rank order.
-// rows_grad_kernel: a cluster of S CTAs per (128 columns, slot) deals out the slot's units of 64 rows and adds its partial
-// sums the same way.
+// rows_shrink_kernel: u and v.  An item is a piece (up to 128 rows of one segment, counted from the segment's first row: a TMA box
+// may begin at any row, so no row of another segment is in it but behind its end) of x or of dy, its work the steps of 128 columns.
+// rows_grad_kernel: dA and dB.  An item is (slot, 128 columns of x or dy), its work the slot's pieces.
+// A step of either is a tile of 128 rows x 128 columns.
+// In both the work of all items stands in one line that is cut into equal parts, one per SM; a CTA walks its part without a pause
+// between items.  An item that the cuts divide is joined in device memory: every CTA writes its partial result, and the last one to
+// arrive adds them in the order of the parts, so the bits do not depend on who that is.  (A form with a cluster per item and an
+// exchange through distributed shared memory spent 10 us per CTA on setting up and joining.)
 //
-// Both are rings of tiles of x or dy as TMA brings them in, multiplied by tcgen05.  8-bit tiles pass through the registers of
-// four warps, which write them as bf16 (exact: the scales are powers of two) in the swizzled order of the tensor cores.  The
-// second product contracts over tokens: the tile [token][64 columns] is an operand whose contiguous index is the output's
-// (M-major), which the descriptor says; nothing is transposed.
+// Both are rings of tiles of x or dy as TMA brings them in, multiplied by tcgen05 into one of two accumulators.  Roles: a producer of tiles,
+// which also tells the others what a stage holds, and one of the other operand (one thread for both would be the slowest role); an issuer; four warps that finish items while the next one is multiplied; two
+// groups of eight warps that take 8-bit tiles in turn through their registers and write them back in place as bf16 (exact: the
+// scales are powers of two) in the swizzled order of the tensor cores.  The second product contracts over tokens: the tile
+// [token][64 columns] is an operand whose contiguous index is the output's (M-major), which the descriptor says; nothing is
+// transposed.
 //
-// dA and dB are fp32 and so are u and v on the way: each goes into the second product as two bf16 values (hi, lo) whose sum is
-// the fp32 value to 2^-17, side by side as 2r columns of one product.  One bf16 value would leave 2^-9, 1e-3 of every gradient.
+// dA and dB are fp32 and so are u and v on the way: each goes into the second product as three bf16 values whose sum is the fp32
+// value, side by side as 3r columns of one product.  One bf16 value would leave 2^-9, 1e-3 of every gradient, two 3e-6.
 //
 // Bound by memory: x and dy leave HBM once (the second pass finds them in L2 up to about 100 MB).
 #include <cstring>
@@ -26,41 +31,67 @@ namespace lml {
 
 using namespace ptx;
 
-constexpr int kRgThreads = 192;                 // producer, issuer, four warps that convert and finish
-constexpr int kRgTile = 128 * 128;              // bytes of a multiplied tile: 128 x 64 bf16 (first pass), 2 x 64 x 64 (second)
-constexpr int kRgRaw = 128 * 64;                // ... of the 8-bit tile it is made of
-constexpr int kRgHalf = 2 * kRankPad * 128;     // bytes of u (or v) of 64 tokens: hi rows, lo rows, 64 tokens each
-constexpr int kRgPiece = 2 * kRgHalf;
-constexpr int kRgMaxStages = 4;
-constexpr int kRgList = 192;                    // segments of a slot looked at a time
+constexpr int kRgGroup = 8;                     // warps of a converting group
+constexpr int kRgFinish = 4;                    // warps that finish items (warps 2 ... 5: one per quarter of the accumulator's lanes)
+constexpr int kRgOther = 2 + kRgFinish;         // the warp that brings in the other operand
+constexpr int kRgFirstConv = kRgOther + 1;
+constexpr int kRgThreads = 32 * (kRgFirstConv + 2 * kRgGroup);
+constexpr int kRgSegs = 320;                    // segments of a launch; a call of more runs in slices
+constexpr int kRgTile = 128 * 128 * 2;          // bytes of a tile as it is multiplied: two halves of 64 columns, [half][row][64]
+constexpr int kRgHalfTile = kRgTile / 2;
+constexpr int kRgRaw = 128 * 128;               // ... of the 8-bit tile it is made of, [row][128]
+constexpr int kRgPiece = 2 * 3 * kRankPad * 128;   // u (or v) of a piece: [64 tokens each][three parts][column][64]
+constexpr int kRgPartial = kRankPad * 128;      // floats of a partial result
+constexpr int kRgMaxStages = 6;
+constexpr int kRgTurns = 16;                    // tiles on their way to and from the converting warps: as many as stages, and two ends
+static_assert(kRgTurns >= kRgMaxStages + 2 && (kRgTurns & (kRgTurns - 1)) == 0, "a turn's place must have been read before it is used again");
+constexpr int kRgWords = 136;                   // scale words of a tile, one per row, brought in from a 16-byte boundary on
+constexpr int kRgLeast = 4;                     // steps of a CTA's part (of a whole pass, if it has fewer)
 
 struct alignas(64) RowsGradParams {
-    CUtensorMap map[2];       // x, dy: boxes of 64 columns x 64 rows
-    CUtensorMap low[2];       // the packed A of the table, B^T of the transposed one
+    CUtensorMap map[2];       // x, dy: boxes of 64 columns (8-bit x: 128) x 128 rows
+    CUtensorMap low[2][kRankPad / kChunk];   // the packed A of the table, B^T of the transposed one: boxes of 64 columns x 16, 32, 48, 64 rows
     SlotSnapshot snap[2];     // table, transposed table
     const uint32_t* scales;   // of x
-    const int32_t *seg_offsets, *ids, *ids_T;
+    const int32_t *seg_offsets, *ids, *ids_T;   // of this slice
+    const int* bad;           // or null: not 0 if the arrays of the call do not hold together (calls of several slices)
     uint32_t* status[2];
     uint8_t* pieces[2];       // u, v
+    float* partial;           // [CTA][2]: of the item that its part begins in, of the item that its part ends in
+    int* arrived;             // [CTA]: of the item that its part ends in and the next one goes on with; zero between calls
     float* out[2];            // dA, dB
-    int d[2];                 // d_in, d_out
-    int T, G, format, r16, stages, S, accumulate, tiles0;
+    int d[2], tiles[2];       // d_in, d_out; in tiles of 128 columns
+    int T, G, r16, ring, accumulate, all_tiles, whole_items;
+    int check_first, check_last;   // the slice begins, ends the call
     unsigned long long live;  // slots with an adapter
 };
 
+// What the producer says about a stage.
+constexpr int kRgFirst = 1, kRgLast = 2, kRgEnd = 4, kRgTouched = 8;   // first, last of an item; last of this CTA; goes through the converting warps
+struct RgInfo {
+    int flags, valid;   // rows
+    int r16;            // columns of the other operand (second pass: of each of its three parts)
+    int word;           // of a converted tile: place of its first scale word; -1: only rows behind the last are cleared
+};
+struct RgTurn { int stage, phase; };   // stage < 0: no more
+
 struct RgCtrl {
-    unsigned long long full[kRgMaxStages], made[kRgMaxStages], empty[kRgMaxStages], done;
+    unsigned long long full[kRgMaxStages], empty[kRgMaxStages], turn[kRgTurns], made[kRgTurns], acc_full[2], acc_free[2];
+    RgInfo info[kRgMaxStages];
+    RgTurn turns[kRgTurns];
     unsigned long long used;
     uint32_t tmem_base;
-    int abort, count[6], n;
-    int first[kRgList], len[kRgList], piece[kRgList];
+    int abort, last, count[kRgSegs / 32], units[kMaxSlots], entry[kMaxSlots];
+    int first[kRgSegs], len[kRgSegs], piece[kRgSegs], pre[kRgSegs + 1];
+    uint8_t slot[2][kRgSegs];
+    alignas(16) uint32_t words[kRgMaxStages][kRgWords];
 };
 
 __device__ __forceinline__ uint64_t umma_desc_m128(uint32_t smem_addr)   // 64 contiguous M per 128-byte swizzled row, rows along K
 {
     uint64_t d = 0;
     d |= (uint64_t)((smem_addr & 0x3FFFFu) >> 4);
-    d |= (uint64_t)(8192 >> 4) << 16;                    // to the next 64 of M
+    d |= (uint64_t)(kRgHalfTile >> 4) << 16;             // to the next 64 of M
     d |= (uint64_t)(1024 >> 4) << 32;                    // to the next 8 of K
     d |= (uint64_t)1 << 46;
     d |= (uint64_t)2 << 61;
@@ -68,493 +99,801 @@ __device__ __forceinline__ uint64_t umma_desc_m128(uint32_t smem_addr)   // 64 c
 }
 constexpr uint32_t kIdescMMajorA = 1u << 15;
 
-// 16 columns of 32 lanes
-__device__ __forceinline__ void tmem_ld_32x16(uint32_t taddr, uint32_t (&r)[16])
+// 4 columns of 32 lanes
+__device__ __forceinline__ void tmem_ld_32x4(uint32_t taddr, uint32_t (&r)[4])
 {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(taddr) : "memory");
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr) : "memory");
 }
-__device__ __forceinline__ float4 ld_peer_v4(uint32_t cluster_addr)
+__device__ __forceinline__ uint2 ld_smem_v2(uint32_t a)
 {
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_addr) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint4 ld_smem_v4(uint32_t a)
-{
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
     return v;
 }
 __device__ __forceinline__ void st_smem_v4(uint32_t a, const uint4& v)
 {
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
-__device__ __forceinline__ void st_smem_f32(uint32_t a, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(a), "f"(v) : "memory"); }
-
-// 16 values of the 8-bit tile at `raw` -> two 16-byte chunks, 2 ch and 2 ch + 1, of the 128-byte row at `row_at` (row: its number, for
-// the swizzle)
-__device__ __forceinline__ void convert16(uint32_t raw, uint32_t row_at, int row, int ch, float s, bool e4m3, bool keep)
+__device__ __forceinline__ float4 ld_cg_v4(const float* p)   // (written by another CTA of this grid)
 {
-    uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
-    if (keep) {
-        const uint4 q = ld_smem_v4(raw);
-        lo = decode8_bf16(make_uint2(q.x, q.y), s, e4m3);
-        hi = decode8_bf16(make_uint2(q.z, q.w), s, e4m3);
-    }
-    st_smem_v4(row_at + (uint32_t)(((2 * ch) ^ (row & 7)) * 16), lo);
-    st_smem_v4(row_at + (uint32_t)(((2 * ch + 1) ^ (row & 7)) * 16), hi);
+    float4 v;
+    asm volatile("ld.global.cg.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ void finish_barrier() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kRgFinish) : "memory"); }
+// Of a converting group; whether any thread says so.
+__device__ __forceinline__ bool group_any(int group, bool v)
+{
+    int r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.s32 p, %1, 0;\n\tbar.red.or.pred q, %2, %3, p;\n\tselp.s32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"(v ? 1 : 0), "r"(2 + group), "n"(32 * kRgGroup) : "memory");
+    return r != 0;
 }
 
-// Whether segment g's two bindings name one adapter in both tables.
+// Whether a segment's two bindings name one adapter in both tables.
 __device__ __forceinline__ bool paired(const RowsGradParams& p, int s, int sT)
 {
     const int r = slot_rank(p.snap[0], s);
     return r > 0 && r == slot_rank(p.snap[1], sT);
 }
 
-__device__ __forceinline__ void rg_setup(RgCtrl* c, int stages, int warp, int tid, uint32_t cols)
+__device__ __forceinline__ void rg_setup(RgCtrl* c, int warp, int tid, uint32_t cols)
 {
     if (tid == 0) {
         c->abort = 0;
         c->used = 0ull;
-        for (int i = 0; i < stages; ++i) {
-            mbar_init(smem_u32(&c->full[i]), 1);
-            mbar_init(smem_u32(&c->made[i]), 4);
+        for (int i = 0; i < kRgMaxStages; ++i) {
+            mbar_init(smem_u32(&c->full[i]), 2);
             mbar_init(smem_u32(&c->empty[i]), 1);
         }
-        mbar_init(smem_u32(&c->done), 1);
+        for (int i = 0; i < kRgTurns; ++i) {
+            mbar_init(smem_u32(&c->turn[i]), 1);
+            mbar_init(smem_u32(&c->made[i]), kRgGroup);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&c->acc_full[i]), 1);
+            mbar_init(smem_u32(&c->acc_free[i]), kRgFinish);
+        }
         fence_mbar_init();
     }
     if (warp == 1) tmem_alloc(smem_u32(&c->tmem_base), cols);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    grid_launch_dependents();   // (after the allocation: what starts from here on may want TMEM and waits for this grid)
-    grid_dependency_wait();
 }
-__device__ __forceinline__ uint32_t tmem_cols_for(int n) { return n <= 32 ? 32u : n <= 64 ? 64u : 128u; }
+__device__ __forceinline__ uint32_t tmem_cols_for(int n) { return n <= 32 ? 32u : n <= 64 ? 64u : n <= 128 ? 128u : n <= 256 ? 256u : 512u; }
 
-__global__ void __launch_bounds__(kRgThreads) rows_shrink_kernel(const __grid_constant__ RowsGradParams p)
+// The ring of a CTA: stages of a tile beside the other operand (of the widest adapter).  Every role walks it with a cursor of its own (a
+// division per step to find the stage costs as much as the step's products).
+struct RgRing {
+    uint32_t base, stage_bytes;
+    int stages;
+    __device__ RgRing(uint32_t at, int bytes, uint32_t low) : base(at), stage_bytes(kRgTile + low), stages(min(bytes / (int)(kRgTile + low), kRgMaxStages)) {}
+};
+struct RgCursor {
+    const RgRing& ring;
+    int i = 0, stage = 0, turn = 0;   // turn: tiles that the converting warps have had to do with
+    uint32_t phase = 0, at;           // of the stage's barriers; its address
+    __device__ explicit RgCursor(const RgRing& r) : ring(r), at(r.base) {}
+    __device__ void advance()
+    {
+        ++i;
+        at += ring.stage_bytes;
+        if (++stage == ring.stages) { stage = 0; phase ^= 1u; at = ring.base; }
+    }
+};
+__device__ __forceinline__ uint32_t turn_phase(int turn) { return (uint32_t)(turn / kRgTurns) & 1u; }
+
+// Producer (one thread): hands a stage, what it holds being written, on to the converting warps; stage -1: there is no more.
+__device__ __forceinline__ void post_turn(RgCtrl* c, int turn, int stage, uint32_t phase)
+{
+    c->turns[turn % kRgTurns] = {stage, (int)phase};
+    mbar_arrive(smem_u32(&c->turn[turn % kRgTurns]));   // (releases what was written)
+}
+// Producer of tiles (one thread): the tile at (row, column) into the stage.  `words`: the scale words of the tile's rows.  A bulk copy wants 16-byte boundaries, so theirs begins up to three words early, and takes kRgWords; where that
+// would reach behind the array's end, ordinary loads bring the rest.
+__device__ __forceinline__ void load_tile(RgCtrl* c, const CUtensorMap* map, uint32_t at, int stage, bool raw, int row, int column, int valid, int flags, int r16,
+                                          const uint32_t* words, const uint32_t* words_end)
+{
+    const uint32_t bar = smem_u32(&c->full[stage]);
+    if (raw) {
+        const uintptr_t addr = reinterpret_cast<uintptr_t>(words);
+        const uint32_t* from = reinterpret_cast<const uint32_t*>(addr & ~(uintptr_t)15);
+        c->info[stage] = {flags, valid, r16, (int)(addr >> 2) & 3};
+        uint32_t bytes = kRgWords * 4;
+        if (words_end - from < kRgWords) {
+            bytes = (uint32_t)(words_end - from) * 4u & ~15u;
+            for (const uint32_t* w = from + bytes / 4; w < words_end; ++w) c->words[stage][w - from] = ld_after_wait(w);
+        }
+        mbar_arrive_expect_tx(bar, kRgRaw + bytes);
+        tma_load_2d(at, map, bar, column / 2, row);   // (8-bit columns in pairs)
+        if (bytes) bulk_load(smem_u32(c->words[stage]), from, bytes, bar);
+    } else {
+        c->info[stage] = {flags, valid, r16, -1};
+        mbar_arrive_expect_tx(bar, kRgTile);
+        tma_load_2d(at, map, bar, column, row);
+        tma_load_2d(at + kRgHalfTile, map, bar, column + 64, row);
+    }
+}
+
+// Issuer of both passes: the steps as they come, told apart by what the producer says about them.  The tile's rows are the product's (first
+// pass: K-major) or contracted (second: M-major).
+template <bool SECOND>
+__device__ __forceinline__ void issue_steps(RgCtrl* c, const RgRing& ring, uint32_t tmem, uint32_t acc_cols, volatile int* abort)   // (one thread)
+{
+    RgCursor u(ring);
+    uint32_t items = 0;
+    int flags;
+    do {
+        if (!mbar_wait(smem_u32(&c->full[u.stage]), u.phase, abort)) return;
+        const RgInfo info = c->info[u.stage];
+        flags = info.flags;
+        const uint32_t buf = items & 1u, acc = tmem + buf * acc_cols, fresh = flags & kRgFirst ? 0u : 1u;
+        if (!fresh && items >= 2 && !mbar_wait(smem_u32(&c->acc_free[buf]), ((items >> 1) & 1u) ^ 1u, abort)) return;
+        if (flags & kRgTouched) {
+            if (!mbar_wait(smem_u32(&c->made[u.turn % kRgTurns]), turn_phase(u.turn), abort)) return;
+            ++u.turn;
+        }
+        tc_fence_after();
+        const uint32_t low = u.at + kRgTile;
+        if (SECOND) {
+            const uint32_t idesc = umma_idesc_bf16(128, 3 * info.r16) | kIdescMMajorA;
+            const uint64_t ad = umma_desc_m128(u.at), bd = umma_desc_k128(low), bd2 = umma_desc_k128(low + (uint32_t)info.r16 * 384u);
+            if (info.valid > kTileM - 16) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) umma_bf16(acc, ad + (uint64_t)(k * (2048 >> 4)), (k < 4 ? bd : bd2) + (uint64_t)((k & 3) * 2), idesc, k > 0 ? 1u : fresh);
+            } else {
+                for (int k = 0; k * 16 < info.valid; ++k) umma_bf16(acc, ad + (uint64_t)(k * (2048 >> 4)), (k < 4 ? bd : bd2) + (uint64_t)((k & 3) * 2), idesc, k > 0 ? 1u : fresh);
+            }
+        } else {
+            const uint32_t idesc = umma_idesc_bf16(128, info.r16);
+            const uint64_t ad = umma_desc_k128(u.at), ad2 = umma_desc_k128(u.at + kRgHalfTile);
+            const uint64_t bd = umma_desc_k128(low), bd2 = umma_desc_k128(low + (uint32_t)info.r16 * 128u);
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                umma_bf16(acc, (k < 4 ? ad : ad2) + (uint64_t)((k & 3) * 2), (k < 4 ? bd : bd2) + (uint64_t)((k & 3) * 2), idesc, k > 0 ? 1u : fresh);
+        }
+        umma_commit(smem_u32(&c->empty[u.stage]));
+        if (flags & kRgLast) {
+            umma_commit(smem_u32(&c->acc_full[buf]));
+            ++items;
+        }
+        u.advance();
+    } while (!(flags & kRgEnd));
+}
+
+// Converting group of both passes: every second tile that is handed on.  Rows behind the last become zeros (in a bf16 tile those that share
+// a step of 16 with it: another token's values times zero would be NaN where they are not finite).
+template <bool E4M3>
+__device__ __forceinline__ void convert_tiles(RgCtrl* c, const RgRing& ring, int group, int wt, int lane, volatile int* abort)
+{
+    const int ch = wt & 3, odd = (wt >> 2) & 1, row0 = wt >> 3, shift = 8 * ((wt & 7) >> 1);
+    const uint32_t to0 = (uint32_t)(odd * kRgHalfTile + row0 * 128 + (((2 * ch + odd) ^ (row0 & 7)) * 16));   // (32 rows on, the swizzle is the same)
+    for (int turn = group;; turn += 2) {
+        const int k = turn % kRgTurns;
+        bool ok = mbar_wait_warp(smem_u32(&c->turn[k]), turn_phase(turn), abort);
+        __syncwarp();
+        const RgTurn what = c->turns[k];
+        if (ok && what.stage < 0) return;
+        const int stage = what.stage < 0 ? 0 : what.stage;
+        ok = ok && mbar_wait_warp(smem_u32(&c->full[stage]), (uint32_t)what.phase, abort);
+        __syncwarp();
+        const uint32_t at = ring.base + (uint32_t)stage * ring.stage_bytes;
+        const RgInfo info = c->info[stage];
+        // 16 values of a row: the 16-byte chunks 2 ch and 2 ch + 1 (of eight) of a half's row, swizzled by the row.  Lanes of the second half
+        // take the odd chunk first, so that the two halves' lanes, which are 16 KB apart, do not meet on a bank.
+        uint2 v[4][2];
+        uint32_t byte[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t from = at + (uint32_t)(q * (kRgRaw / 4) + wt * 16);
+            v[q][0] = ld_smem_v2(from + odd * 8);
+            v[q][1] = ld_smem_v2(from + 8 - odd * 8);
+            byte[q] = (c->words[stage][(info.word & 3) + row0 + 32 * q] >> shift) & 0xffu;
+        }
+        const bool usual = info.valid == kTileM && max(max(byte[0], byte[1]), max(byte[2], byte[3])) <= Decoder<E4M3>::kMost;
+        if (group_any(group, !ok)) return;   // (everybody has the tile's values, so their place may be written; or a wait gave up)
+        const uint32_t to = at + to0;
+        if (info.word >= 0 && usual) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const Decoder<E4M3> decode(byte[q]);
+                st_smem_v4(to + (uint32_t)(q * 32 * 128), decode.eight(v[q][0]));
+                st_smem_v4((to ^ 16u) + (uint32_t)(q * 32 * 128), decode.eight(v[q][1]));
+            }
+        } else if (info.word >= 0) {
+#pragma unroll 1
+            for (int q = 0; q < 4; ++q) {
+                const bool there = row0 + 32 * q < info.valid;
+                const uint4 zero = make_uint4(0, 0, 0, 0);
+                st_smem_v4(to + (uint32_t)(q * 32 * 128), there ? decode8<E4M3>(v[0][0], byte[0]) : zero);
+                st_smem_v4((to ^ 16u) + (uint32_t)(q * 32 * 128), there ? decode8<E4M3>(v[0][1], byte[0]) : zero);
+#pragma unroll
+                for (int i = 0; i < 3; ++i) { v[i][0] = v[i + 1][0]; v[i][1] = v[i + 1][1]; byte[i] = byte[i + 1]; }
+            }
+        } else {
+            const int rows = 16 - (info.valid & 15);
+            for (int e = wt; e < rows * 16; e += 32 * kRgGroup) {
+                const int row = info.valid + (e >> 4);
+                st_smem_v4(at + ((e >> 3) & 1) * kRgHalfTile + row * 128 + (e & 7) * 16, make_uint4(0, 0, 0, 0));
+            }
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&c->made[k]));
+    }
+}
+
+// The line of work: W steps, P parts; part k begins at W k / P.  (W: 32 KB of activations each, so 31 bits are enough.)
+struct RgLine {
+    int W, P;
+    __device__ RgLine(int w) : W(w), P(max(1, min((int)gridDim.x, w / kRgLeast))) {}
+    __device__ int begin(int k) const { return k < P ? (int)((long long)W * k / P) : W; }
+    __device__ int part_of(int w) const { return (int)(((long long)(w + 1) * P - 1) / W); }   // the last part that begins at or before w
+};
+// An item that several parts share: its first and last part, and where this one leaves its result.
+struct RgShare { int first, last, slot; };
+__device__ __forceinline__ RgShare share_of(const RgLine& line, int item, int n, int k)
+{
+    const int first = line.part_of(item);
+    return {first, line.part_of(item + n - 1), k == first ? 1 : 0};   // (the others begin behind the item's first step)
+}
+// After all finishing warps have written this CTA's partial result: whether it is the last one of the item's.
+__device__ __forceinline__ bool arrive_last(RgCtrl* c, const RowsGradParams& p, const RgShare& s)
+{
+    __threadfence();
+    finish_barrier();
+    if (threadIdx.x == 64) {   // (the first of them)
+        const int n = atomicAdd(p.arrived + s.first, 1);
+        c->last = n == s.last - s.first;
+        if (c->last) atomicExch(p.arrived + s.first, 0);   // (for the next call)
+        __threadfence();
+    }
+    finish_barrier();
+    return c->last != 0;
+}
+// Four values of the joined result: up to eight parts' loads in flight
+__device__ __forceinline__ float4 join(const RowsGradParams& p, const RgShare& s, int at)
+{
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k0 = s.first; k0 <= s.last; k0 += 8) {
+        float4 w[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (k0 + q <= s.last) w[q] = ld_cg_v4(p.partial + (size_t)(2 * (k0 + q) + (k0 + q == s.first ? 1 : 0)) * kRgPartial + at);
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if (k0 + q <= s.last) { v.x += w[q].x; v.y += w[q].y; v.z += w[q].z; v.w += w[q].w; }
+    }
+    return v;
+}
+
+// A segment of the slice, this thread's.  Returns whether the slice's arrays are malformed (the same in all threads).
+struct RgSeg { int s0 = 0, s1 = 0, s = -1, sT = -1; bool mine = false; };
+__device__ __forceinline__ bool load_segment(const RowsGradParams& p, int g, RgSeg& seg)
+{
+    int bad = 0;
+    if (g < p.G) {
+        seg.s0 = ld_after_wait(p.seg_offsets + g);
+        seg.s1 = ld_after_wait(p.seg_offsets + g + 1);
+        seg.s = ld_after_wait(p.ids + g);
+        seg.sT = ld_after_wait(p.ids_T + g);
+        if (seg.s1 < seg.s0 || seg.s0 < 0 || seg.s1 > p.T) bad = 1;
+        if ((p.check_first && g == 0 && seg.s0 != 0) || (p.check_last && g == p.G - 1 && seg.s1 != p.T)) bad = 1;
+        seg.mine = seg.s1 > seg.s0 && paired(p, seg.s, seg.sT);
+    }
+    if (p.bad && g == 0 && ld_after_wait(p.bad)) bad = 1;
+    return __syncthreads_or(bad) != 0;
+}
+__device__ __forceinline__ void flag_segment(const RowsGradParams& p, const RgSeg& seg)
+{
+    if (seg.s1 <= seg.s0 || (seg.s == -1 && seg.sT == -1)) return;
+    const int r = slot_rank(p.snap[0], seg.s);
+    if (r == 0) atomicOr(p.status[0], LML_FLAG_BAD_SLOT);
+    if (slot_rank(p.snap[1], seg.sT) != r) atomicOr(p.status[1], LML_FLAG_BAD_SLOT);
+}
+
+// ---- first pass ------------------------------------------------------------------------------------------
+// This CTA's part of the line, item by item: pieces in order, of each x, then dy.
+struct ShrinkTasks {
+    const RowsGradParams& p;
+    const RgCtrl* c;
+    int w, end;
+    int e = 0;
+    int job = 0, step = 0, n = 0, row = 0, valid = 0, piece = 0, slot = 0;
+    __device__ ShrinkTasks(const RowsGradParams& p_, const RgCtrl* c_, int w0, int w1) : p(p_), c(c_), w(w0), end(w1) {}
+    __device__ bool next()
+    {
+        w += n;
+        if (w >= end) return false;
+        const int both = p.tiles[0] + p.tiles[1], idx = w / both, in = w - idx * both;
+        job = in >= p.tiles[0] ? 1 : 0;
+        step = in - (job ? p.tiles[0] : 0);
+        n = min(p.tiles[job] - step, end - w);
+        while (c->pre[e + 1] <= idx) ++e;
+        const int i = idx - c->pre[e];
+        row = c->first[e] + i * kTileM;
+        valid = min(c->len[e] - i * kTileM, kTileM);
+        piece = c->piece[e] + i;
+        slot = c->slot[job][e];
+        return true;
+    }
+    __device__ bool whole() const { return n == p.tiles[job]; }
+    __device__ int item() const { return w - step; }
+};
+
+// Three bf16 values whose sum is x; an x that is not finite stands in the first alone.
+__device__ __forceinline__ void split3(float x, float (&part)[3])
+{
+    part[0] = __bfloat162float(__float2bfloat16_rn(x));
+    const float rest = fabsf(part[0]) < INFINITY ? x - part[0] : 0.f;
+    part[1] = __bfloat162float(__float2bfloat16_rn(rest));
+    part[2] = rest - part[1];
+}
+
+template <int FMT>
+__global__ void __launch_bounds__(kRgThreads, 1) rows_shrink_kernel(const __grid_constant__ RowsGradParams p)
 {
     extern __shared__ uint8_t rg_smem[];
     __shared__ RgCtrl ctrl;
     RgCtrl* c = &ctrl;
-    const uint32_t ring = (smem_u32(rg_smem) + 1023u) & ~1023u;
+    const uint32_t smem = (smem_u32(rg_smem) + 1023u) & ~1023u;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int job = blockIdx.y, S = p.S, rank = (int)cluster_ctarank();
-    const int b = (int)(blockIdx.x / (unsigned)S);
-    const uint32_t cols = tmem_cols_for(p.r16);
-    rg_setup(c, p.stages, warp, tid, cols);
+    const uint32_t cols = tmem_cols_for(2 * p.r16);
+    rg_setup(c, warp, tid, cols);
+    // (After the allocation: what starts from here on may want TMEM and waits for this grid.  And after the wait: rows_grad_kernel
+    // takes it that whatever came before this grid is complete.)
+    grid_dependency_wait();
+    grid_launch_dependents();
     const uint32_t tmem = c->tmem_base;
     volatile int* abort = &c->abort;
 
-    // One CTA checks the arrays for the whole call.
-    if (blockIdx.x == 0 && job == 0) {
-        uint32_t f = 0, fT = 0;
-        for (int g = tid; g < p.G; g += kRgThreads) {
-            const int s0 = ld_after_wait(p.seg_offsets + g), s1 = ld_after_wait(p.seg_offsets + g + 1);
-            if (s1 < s0 || s0 < 0 || s1 > p.T) f |= LML_FLAG_BAD_OFFSETS;
-            const int s = ld_after_wait(p.ids + g), sT = ld_after_wait(p.ids_T + g);
-            if (s1 <= s0 || (s == -1 && sT == -1)) continue;
-            if (slot_rank(p.snap[0], s) == 0) f |= LML_FLAG_BAD_SLOT;
-            if (slot_rank(p.snap[1], sT) != slot_rank(p.snap[0], s)) fT |= LML_FLAG_BAD_SLOT;
-        }
-        if (tid == 0 && (ld_after_wait(p.seg_offsets) != 0 || ld_after_wait(p.seg_offsets + p.G) != p.T)) f |= LML_FLAG_BAD_OFFSETS;
-        if (f) atomicOr(p.status[0], f);
-        if (fT) atomicOr(p.status[1], fT);
+    // The slice's pieces, counted through its segments.
+    RgSeg seg;
+    const bool bad = load_segment(p, tid, seg);
+    if (blockIdx.x == 0) {
+        flag_segment(p, seg);
+        if (bad && tid == 0) atomicOr(p.status[0], LML_FLAG_BAD_OFFSETS);
     }
+    const int mine = seg.mine && !bad ? (seg.s1 - seg.s0 + kTileM - 1) / kTileM : 0;
+    int upto = mine;
+#pragma unroll
+    for (int m = 1; m < 32; m <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, upto, m);
+        if (lane >= m) upto += v;
+    }
+    if (tid < kRgSegs && lane == 31) c->count[warp] = upto;
+    __syncthreads();
+    if (tid < kRgSegs) {
+        for (int k = 0; k < warp; ++k) upto += c->count[k];
+        c->first[tid] = seg.s0; c->len[tid] = seg.s1 - seg.s0; c->piece[tid] = seg.s0 / kTileM + tid;
+        c->slot[0][tid] = (uint8_t)seg.s; c->slot[1][tid] = (uint8_t)seg.sT;
+        c->pre[tid + 1] = upto;
+        if (tid == 0) c->pre[0] = 0;
+    }
+    __syncthreads();
+    const RgLine line(c->pre[kRgSegs] * (p.tiles[0] + p.tiles[1]));
+    const int w0 = line.begin((int)blockIdx.x), w1 = line.begin((int)blockIdx.x + 1);
 
-    // Piece b: the largest g whose first piece, s0 / 128 + g, is not behind b.  (Pieces of a segment are never more than lie
-    // between its first and the next one's; the arrays may be malformed, so everything is clamped.)
-    int p0 = 0, valid = 0, slot = -1;
-    {
-        int lo = 0, hi = p.G;
-        if (p.G <= kRgList) {
-            for (int g = tid; g < p.G; g += kRgThreads) c->first[g] = ld_after_wait(p.seg_offsets + g);
-            __syncthreads();
-        }
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            const int s0 = p.G <= kRgList ? c->first[mid] : ld_after_wait(p.seg_offsets + mid);
-            if (mid + s0 / kTileM <= b) lo = mid; else hi = mid;
-        }
-        const long long s0 = ld_after_wait(p.seg_offsets + lo), s1 = ld_after_wait(p.seg_offsets + lo + 1);
-        const long long first = s0 + (b - (s0 / kTileM + lo)) * (long long)kTileM, end = s1 < p.T ? s1 : p.T;
-        const int s = ld_after_wait(p.ids + lo), sT = ld_after_wait(p.ids_T + lo);
-        if (s0 >= 0 && first >= s0 && first < end && paired(p, s, sT)) {
-            p0 = (int)first;
-            valid = (int)(end - first < kTileM ? end - first : kTileM);
-            slot = job == 0 ? s : sT;
-        }
-    }
-    if (valid > 0) {   // (the same in all CTAs of the cluster)
-        const SlotSnapshot& snap = p.snap[job];
-        const int r = snap.rank[slot], r16 = chunks_of_rank(r) * kChunk;
-        const int nkb = (p.d[job] + 63) / 64, kb0 = nkb * rank / S, n = nkb * (rank + 1) / S - kb0;
-        const bool raw = job == 0 && p.format != kBf16;
-        const uint32_t low_bytes = (uint32_t)p.r16 * 128u, stage_bytes = kRgTile + low_bytes + (p.format != kBf16 ? kRgRaw : 0);
+    const RgRing ring(smem, p.ring, (uint32_t)p.r16 * 256u);
+    if (w0 < w1) {
         if (warp == 0) {
             if (elect_one()) {
-                for (int i = 0; i < n; ++i) {
-                    const int st = i % p.stages;
-                    if (!mbar_wait(smem_u32(&c->empty[st]), ((i / p.stages) & 1) ^ 1, abort)) break;
-                    const uint32_t at = ring + st * stage_bytes, bar = smem_u32(&c->full[st]);
-                    const int k = (kb0 + i) * 64, boxes = valid > 64 ? 2 : 1;
-                    mbar_arrive_expect_tx(bar, (uint32_t)(r16 * 128 + boxes * (raw ? kRgRaw / 2 : kRgTile / 2)));
-                    for (int h = 0; h < boxes; ++h) {
-                        if (raw) tma_load_2d(at + kRgTile + low_bytes + h * (kRgRaw / 2), &p.map[job], bar, k / 2, p0 + h * 64);
-                        else tma_load_2d(at + h * (kRgTile / 2), &p.map[job], bar, k, p0 + h * 64);
+                RgCursor u(ring);
+                const uint32_t* words_end = p.scales + (size_t)kept_groups(p.d[0]) * p.T;
+                for (ShrinkTasks t(p, c, w0, w1); t.next();) {
+                    const bool raw = FMT != kBf16 && t.job == 0;
+                    const uint32_t* words = p.scales + (size_t)t.step * p.T + t.row;
+                    const CUtensorMap* map = &p.map[t.job];
+                    const int r16 = chunks_of_rank(p.snap[t.job].rank[t.slot]) * kChunk, end = t.w + t.n == w1 ? kRgLast | kRgEnd : kRgLast;
+                    int flags = kRgFirst | (raw ? kRgTouched : 0), k = t.step * 128;
+                    for (int left = t.n; left > 0; --left, k += 128, words += p.T, u.advance()) {
+                        if (!mbar_wait(smem_u32(&c->empty[u.stage]), u.phase ^ 1u, abort)) break;
+                        if (left == 1) flags |= end;
+                        load_tile(c, map, u.at, u.stage, raw, t.row, k, t.valid, flags, r16, words, words_end);
+                        if (raw) { post_turn(c, u.turn, u.stage, u.phase); ++u.turn; }
+                        flags &= ~kRgFirst;
                     }
-                    for (int j = 0; j < r16; j += kChunk) tma_load_3d(at + kRgTile + j * 128, &p.low[job], bar, k, j, slot);
+                }
+                if (FMT != kBf16)
+                    for (int k = 0; k < 2; ++k) post_turn(c, u.turn + k, -1, 0);
+            }
+        } else if (warp == kRgOther) {
+            if (elect_one()) {
+                RgCursor u(ring);
+                for (ShrinkTasks t(p, c, w0, w1); t.next();) {
+                    const int chunks = chunks_of_rank(p.snap[t.job].rank[t.slot]), row = t.slot * kRankPad;
+                    const uint32_t half = (uint32_t)chunks * kChunk * 128u;
+                    const CUtensorMap* low = &p.low[t.job][chunks - 1];
+                    int k = t.step * 128;
+                    for (int left = t.n; left > 0; --left, k += 128, u.advance()) {
+                        if (!mbar_wait(smem_u32(&c->empty[u.stage]), u.phase ^ 1u, abort)) break;
+                        const uint32_t bar = smem_u32(&c->full[u.stage]);
+                        mbar_arrive_expect_tx(bar, 2 * half);
+                        tma_load_2d(u.at + kRgTile, low, bar, k, row);
+                        tma_load_2d(u.at + kRgTile + half, low, bar, k + 64, row);
+                    }
                 }
             }
         } else if (warp == 1) {
-            if (elect_one()) {
-                const uint32_t idesc = umma_idesc_bf16(128, r16);
-                bool ok = true;
-                for (int i = 0; i < n; ++i) {
-                    const int st = i % p.stages;
-                    ok = mbar_wait(smem_u32(&c->full[st]), (i / p.stages) & 1, abort) && (!raw || mbar_wait(smem_u32(&c->made[st]), (i / p.stages) & 1, abort));
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint32_t at = ring + st * stage_bytes;
-                    const uint64_t ad = umma_desc_k128(at), bd = umma_desc_k128(at + kRgTile);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) umma_bf16(tmem, ad + (uint64_t)(k * 2), bd + (uint64_t)(k * 2), idesc, (i > 0 || k > 0) ? 1u : 0u);
-                    umma_commit(smem_u32(&c->empty[st]));
-                }
-                if (ok && n > 0) umma_commit(smem_u32(&c->done));
-            }
-        } else if (raw) {
-            const int wt = tid - 64, ch = wt & 3;
-            const bool e4m3 = p.format == kE4m3;
-            uint32_t word[4], next[4];
-            auto fetch = [&](int i, uint32_t (&w)[4]) {
-                const long long cg = (kb0 + i) >> 1;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int row = q * 32 + (wt >> 2);
-                    w[q] = i < n && row < valid ? ld_after_wait(p.scales + cg * p.T + p0 + row) : 0u;
-                }
-            };
-            fetch(0, next);
-            for (int i = 0; i < n; ++i) {
-                const int st = i % p.stages;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) word[q] = next[q];
-                fetch(i + 1, next);
-                if (!mbar_wait_warp(smem_u32(&c->full[st]), (i / p.stages) & 1, abort)) break;
+            if (elect_one()) issue_steps<false>(c, ring, tmem, (uint32_t)p.r16, abort);
+        } else if (warp < kRgOther) {
+            // (After a wait that gave up these warps go through the rest all the same: the counters of shared items come out right.  The
+            // status word says that the results do not.)
+            const int wt = tid - 64;
+            uint32_t items = 0;
+            for (ShrinkTasks t(p, c, w0, w1); t.next(); ++items) {
+                mbar_wait_warp(smem_u32(&c->acc_full[items & 1]), (items >> 1) & 1, abort);
                 __syncwarp();
-                const uint32_t at = ring + st * stage_bytes;
-                const int byte = ((kb0 + i) & 1) * 2 + (ch >> 1);
+                tc_fence_after();
+                // The products: lane = token.
+                const int r = p.snap[t.job].rank[t.slot], r16 = chunks_of_rank(r) * kChunk, row = (warp & 3) * 32 + lane;
+                const float sc = p.snap[t.job].scale[t.slot];
+                const bool whole = t.whole();
+                const RgShare share = whole ? RgShare{0, 0, 0} : share_of(line, t.item(), p.tiles[t.job], (int)blockIdx.x);
+                uint8_t* out = p.pieces[t.job] + (size_t)t.piece * kRgPiece;
+                float* mine_at = p.partial + (size_t)(2 * blockIdx.x + share.slot) * kRgPartial;
+                // (r16 is a multiple of 16: the swizzle goes by j alone)
+                uint8_t* half = out + (size_t)(row >> 6) * (r16 * 384) + (row & 7) * 2;
+                const bool there = row < t.valid;   // (rows behind the segment, columns behind the rank: whatever they hold)
+                const uint32_t from = tmem + (items & 1) * (uint32_t)p.r16 + ((uint32_t)((warp & 3) * 32) << 16);
+#pragma unroll 1
+                for (int j = 0; j < r16; j += 4) {
+                    uint32_t v[4];
+                    tmem_ld_32x4(from + (uint32_t)j, v);
+                    tmem_ld_wait();
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int row = q * 32 + (wt >> 2);
-                    convert16(at + kRgTile + low_bytes + row * 64 + ch * 16, at + row * 128, row, ch,
-                              scale_of_byte((word[q] >> (8 * byte)) & 0xffu), e4m3, row < valid);
+                    for (int e = 0; e < 4; ++e) {
+                        if (whole) {
+                            float part[3];
+                            split3(there && j + e < r ? __uint_as_float(v[e]) * sc : 0.f, part);
+                            uint8_t* at = half + (j + e) * 128 + ((((row & 63) >> 3) ^ ((j + e) & 7)) * 16);
+#pragma unroll
+                            for (int k = 0; k < 3; ++k) *reinterpret_cast<__nv_bfloat16*>(at + k * r16 * 128) = __float2bfloat16_rn(part[k]);
+                        } else {
+                            mine_at[(j + e) * 128 + row] = __uint_as_float(v[e]);
+                        }
+                    }
                 }
-                fence_proxy_async_smem();
+                tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&c->made[st]));
-            }
-        }
-        __syncwarp();
-        bool ok = true;
-        if (warp >= 2 && n > 0) {
-            ok = mbar_wait_warp(smem_u32(&c->done), 0, abort);
-            if (!ok) __nanosleep(50000);   // gave up: let copies still in flight land before the ring takes the partial sums
-            __syncwarp();
-            tc_fence_after();
-        }
-        // partial products [column][token]: the ring is idle in this CTA from here on
-        if (warp >= 2) {
-            const int row = (warp & 3) * 32 + lane;
-            for (int j = 0; j < r16; j += 16) {
-                uint32_t v[16];
-                tmem_ld_32x16(tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)j, v);
-                tmem_ld_wait();
+                if (lane == 0) mbar_arrive(smem_u32(&c->acc_free[items & 1]));
+                if (!whole && arrive_last(c, p, share)) {
+                    for (int e = wt; e < r16 * 32; e += 32 * kRgFinish) {   // four tokens of one column
+                        const int j = e >> 5, t4 = (e & 31) * 4;
+                        const float4 v = join(p, share, e * 4);
+                        const float x[4] = {v.x, v.y, v.z, v.w};
+                        float part[4][3];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) st_smem_f32(ring + (uint32_t)(((j + e) * 128 + row) * 4), n > 0 && ok ? __uint_as_float(v[e]) : 0.f);
-            }
-            tc_fence_before();
-        }
-        cluster_sync_all();
-        const float sc = snap.scale[slot];
-        uint8_t* out = p.pieces[job] + (size_t)b * kRgPiece;
-        for (int e = rank * kRgThreads + tid; e < r16 * 16; e += S * kRgThreads) {   // eight tokens of one column
-            const int j = e >> 4, t8 = e & 15;
-            float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            for (int q = 0; q < S; ++q) {   // rank order: the sum does not depend on timing
-                const uint32_t from = mapa_shared(ring + (uint32_t)((j * 128 + t8 * 8) * 4), (uint32_t)q);
-                const float4 a = ld_peer_v4(from), d = ld_peer_v4(from + 16);
-                v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
-                v[4] += d.x; v[5] += d.y; v[6] += d.z; v[7] += d.w;
-            }
-            uint32_t hi[4], lo[4];
+                        for (int i = 0; i < 4; ++i) split3(j < r && t4 + i < t.valid ? x[i] * sc : 0.f, part[i]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float x[2], l[2];
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    x[k] = j < r && t8 * 8 + 2 * i + k < valid ? v[2 * i + k] * sc : 0.f;   // (rows behind the segment, columns behind the rank: whatever they hold)
-                    const float h = __bfloat162float(__float2bfloat16_rn(x[k]));
-                    l[k] = fabsf(h) < INFINITY ? x[k] - h : 0.f;
+                        for (int k = 0; k < 3; ++k) {
+                            const int line_at = k * r16 + j;
+                            *reinterpret_cast<uint2*>(out + (size_t)(t4 >> 6) * (r16 * 384) + line_at * 128 + ((((t4 & 63) >> 3) ^ (line_at & 7)) * 16) + (t4 & 4) * 2) =
+                                make_uint2(pack_bf16(part[0][k], part[1][k]), pack_bf16(part[2][k], part[3][k]));
+                        }
+                    }
                 }
-                hi[i] = pack_bf16(x[0], x[1]);
-                lo[i] = pack_bf16(l[0], l[1]);
             }
-            uint8_t* half = out + (size_t)(t8 >> 3) * kRgHalf;
-            const int jl = r16 + j;
-            *reinterpret_cast<uint4*>(half + j * 128 + (((t8 & 7) ^ (j & 7)) * 16)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-            *reinterpret_cast<uint4*>(half + jl * 128 + (((t8 & 7) ^ (jl & 7)) * 16)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+            fence_proxy_async_all();          // the pieces are read by bulk copies
+        } else if (FMT != kBf16) {
+            const int group = (warp - kRgFirstConv) / kRgGroup;
+            convert_tiles<FMT == kE4m3>(c, ring, group, tid - 32 * (kRgFirstConv + group * kRgGroup), lane, abort);
         }
-        fence_proxy_async_all();   // the pieces are read by bulk copies
-        if (tid == 0 && *abort) atomicOr(p.status[0], LML_FLAG_TIMEOUT);
-        cluster_sync_all();        // peers stay until their partial products have been read
     }
+    __syncwarp();
+    if (*abort) __nanosleep(50000);   // gave up: let copies still in flight land before the CTA goes away
     __syncthreads();
+    if (tid == 0 && *abort) atomicOr(p.status[0], LML_FLAG_TIMEOUT);
     if (warp == 1) {
         tc_fence_after();
         tmem_dealloc(tmem, cols);
     }
 }
 
-__global__ void __launch_bounds__(kRgThreads) rows_grad_kernel(const __grid_constant__ RowsGradParams p)
+// ---- second pass -----------------------------------------------------------------------------------------
+// Items: slots in use in order, of each the column tiles (x first, then dy), of each its units.  A CTA has its part of the line, or, if
+// there are few items, whole ones.
+struct GradTasks {
+    const RowsGradParams& p;
+    const RgCtrl* c;
+    unsigned long long mask;   // slots from here on
+    int w, end, base = 0;   // base: of the slot at hand
+    int slot = 0, units = 0, tile = 0, a = 0, b = 0;
+    __device__ GradTasks(const RowsGradParams& p_, const RgCtrl* c_, int w0, int w1) : p(p_), c(c_), mask(c_->used), w(w0), end(w1) {}
+    __device__ void next_slot()
+    {
+        base += units * p.all_tiles;
+        slot = __ffsll((long long)mask) - 1;
+        mask &= mask - 1ull;
+        units = c->units[slot];
+    }
+    __device__ bool next()
+    {
+        if (p.whole_items) {   // w, end, base: items here
+            if (b > 0) w += gridDim.x;
+            if (w >= end) return false;
+            while (units == 0 || w >= base + p.all_tiles) {
+                if (units) base += p.all_tiles;
+                slot = __ffsll((long long)mask) - 1;
+                mask &= mask - 1ull;
+                units = c->units[slot];
+            }
+            tile = (int)(w - base);
+            a = 0; b = units;
+            return true;
+        }
+        w += b - a;
+        if (w >= end) return false;
+        while (w >= base + units * p.all_tiles) next_slot();
+        const int in = w - base;
+        tile = in / units;
+        a = in - tile * units;
+        b = min(units, a + (end - w));
+        return true;
+    }
+    __device__ bool whole() const { return b - a == units; }
+    __device__ bool last() const { return p.whole_items ? w + gridDim.x >= end : w + (b - a) >= end; }   // of this CTA's
+    __device__ int item() const { return w - a; }
+    __device__ int job() const { return tile < p.tiles[0] ? 0 : 1; }
+    __device__ int column() const { return (tile < p.tiles[0] ? tile : tile - p.tiles[0]) * 128; }
+};
+// The pieces of a task, in the order of the slot's segments.
+struct RgPieces {
+    const RgCtrl* c;
+    int e, k, left, first = 0, len = 0, pieces = 0, at0 = 0;   // of the segment at hand
+    __device__ void load()
+    {
+        first = c->first[e];
+        len = c->len[e];
+        pieces = (len + kTileM - 1) / kTileM;
+        at0 = c->piece[e];
+    }
+    __device__ RgPieces(const RgCtrl* c_, const GradTasks& t) : c(c_), left(t.b - t.a)
+    {
+        e = c->entry[t.slot];
+        while (c->pre[e] + (c->len[e] + kTileM - 1) / kTileM <= t.a) ++e;
+        k = t.a - c->pre[e] - 1;
+        load();
+    }
+    __device__ bool next()
+    {
+        if (left-- <= 0) return false;
+        if (++k >= pieces) { ++e; k = 0; load(); }
+        return true;
+    }
+    __device__ int row() const { return first + k * kTileM; }
+    __device__ int valid() const { return min(len - k * kTileM, kTileM); }
+    __device__ size_t at() const { return (size_t)(at0 + k) * kRgPiece; }
+};
+
+template <int FMT>
+__global__ void __launch_bounds__(kRgThreads, 1) rows_grad_kernel(const __grid_constant__ RowsGradParams p)
 {
     extern __shared__ uint8_t rg_smem[];
     __shared__ RgCtrl ctrl;
     RgCtrl* c = &ctrl;
-    const uint32_t ring = (smem_u32(rg_smem) + 1023u) & ~1023u;
+    const uint32_t smem = (smem_u32(rg_smem) + 1023u) & ~1023u;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int S = p.S, rank = (int)cluster_ctarank(), tile = (int)(blockIdx.x / (unsigned)S);
-    const int job = tile < p.tiles0 ? 0 : 1, c0 = (job == 0 ? tile : tile - p.tiles0) * 128;
-    const uint32_t cols = tmem_cols_for(2 * p.r16);
-    rg_setup(c, p.stages, warp, tid, cols);
+    const uint32_t cols = tmem_cols_for(6 * p.r16);
+    if (tid < kMaxSlots) c->units[tid] = 0;
+    rg_setup(c, warp, tid, cols);
+    grid_launch_dependents();   // (after the allocation, see rows_shrink_kernel)
+    // rows_shrink_kernel let this grid go after its own wait, so everything but the pieces that it writes is there already; only the
+    // producer of the other operand waits for it.  (With no tokens nothing went before.)
+    if (p.T == 0) grid_dependency_wait();
     const uint32_t tmem = c->tmem_base;
     volatile int* abort = &c->abort;
 
-    // The slots in use, and whether the arrays hold together (if not, nothing is added).
-    int bad = p.T == 0 ? 1 : 0;
-    for (int g = tid; g < p.G && p.T > 0; g += kRgThreads) {
-        const int s0 = ld_after_wait(p.seg_offsets + g), s1 = ld_after_wait(p.seg_offsets + g + 1);
-        if (s1 < s0 || s0 < 0 || s1 > p.T) bad = 1;
-        const int s = ld_after_wait(p.ids + g);
-        if (s1 > s0 && paired(p, s, ld_after_wait(p.ids_T + g))) atomicOr(&c->used, 1ull << s);
+    // The slice's segments, by slot.
+    RgSeg seg;
+    const bool bad = load_segment(p, tid, seg);
+    const bool mine = seg.mine && !bad;
+    const int mine_units = mine ? (seg.s1 - seg.s0 + kTileM - 1) / kTileM : 0;
+    if (tid < kRgSegs) {
+        c->slot[0][tid] = mine ? (uint8_t)seg.s : (uint8_t)255;
+        c->len[tid] = mine_units;   // (for now)
     }
-    if (tid == 0 && p.T > 0 && (ld_after_wait(p.seg_offsets) != 0 || ld_after_wait(p.seg_offsets + p.G) != p.T)) bad = 1;
-    bad = __syncthreads_or(bad);
-    unsigned long long mask = p.accumulate ? (bad ? 0ull : c->used) : p.live;
-    for (int z = blockIdx.y; z > 0 && mask; --z) mask &= mask - 1ull;
-    if (mask) {   // (the same in all CTAs of the cluster)
-        const int slot = __ffsll((long long)mask) - 1;
-        const int r = p.snap[0].rank[slot], r16 = chunks_of_rank(r) * kChunk;
-        const bool raw = job == 0 && p.format != kBf16;
-        const uint32_t low_bytes = (uint32_t)p.r16 * 256u, stage_bytes = kRgTile + low_bytes + (p.format != kBf16 ? kRgRaw : 0);
-        int it = 0;      // units that this CTA has taken; the same in every role
-        int unit = 0;    // units of the slot before the list's
-        for (int g0 = 0; g0 < p.G && !bad; g0 += kRgThreads) {
-            // the slot's segments among the next 192, in order
-            const int g = g0 + tid;
-            int s0 = 0, s1 = 0;
-            bool mine = false;
-            if (g < p.G && ld_after_wait(p.ids + g) == slot) {
-                s0 = ld_after_wait(p.seg_offsets + g);
-                s1 = ld_after_wait(p.seg_offsets + g + 1);
-                mine = s1 > s0 && paired(p, slot, ld_after_wait(p.ids_T + g));
-            }
-            const uint32_t ballot = __ballot_sync(0xffffffffu, mine);
-            if (lane == 0) c->count[warp] = __popc(ballot);
-            __syncthreads();
-            int before = 0, total = 0;
-#pragma unroll
-            for (int w = 0; w < kRgThreads / 32; ++w) {
-                before += w < warp ? c->count[w] : 0;
-                total += c->count[w];
-            }
-            if (mine) {
-                const int at = before + __popc(ballot & ((1u << lane) - 1u));
-                c->first[at] = s0; c->len[at] = s1 - s0; c->piece[at] = s0 / kTileM + g;
-            }
-            __syncthreads();
-            if (total == 0) continue;
-            // Every role walks the same units: f(row, valid rows, piece, half)
-            auto walk = [&](auto&& f) {
-                int i = it, base = unit;
-                for (int e = 0; e < total; ++e) {
-                    const int units = (c->len[e] + 63) / 64;
-                    int k = rank - base % S;
-                    if (k < 0) k += S;
-                    for (; k < units; k += S, ++i) {
-                        const int left = c->len[e] - k * 64;
-                        if (!f(i, c->first[e] + k * 64, left < 64 ? left : 64, c->piece[e] + (k >> 1), k & 1)) return i;
-                    }
-                    base += units;
-                }
-                return i;
-            };
-            if (warp == 0) {
-                if (elect_one()) {
-                    walk([&](int i, int row, int, int piece, int half) {
-                        const int st = i % p.stages;
-                        if (!mbar_wait(smem_u32(&c->empty[st]), ((i / p.stages) & 1) ^ 1, abort)) return false;
-                        const uint32_t at = ring + st * stage_bytes, bar = smem_u32(&c->full[st]);
-                        mbar_arrive_expect_tx(bar, (uint32_t)(r16 * 256 + (raw ? kRgRaw : kRgTile)));
-                        for (int h = 0; h < 2; ++h) {
-                            if (raw) tma_load_2d(at + kRgTile + low_bytes + h * (kRgRaw / 2), &p.map[job], bar, (c0 + h * 64) / 2, row);
-                            else tma_load_2d(at + h * (kRgTile / 2), &p.map[job], bar, c0 + h * 64, row);
-                        }
-                        // (u for dy, v for x)
-                        bulk_load(at + kRgTile, p.pieces[job ^ 1] + (size_t)piece * kRgPiece + (size_t)half * kRgHalf, (uint32_t)(r16 * 256), bar);
-                        return true;
-                    });
-                }
-            } else if (warp == 1) {
-                if (elect_one()) {
-                    const uint32_t idesc = umma_idesc_bf16(128, 2 * r16) | kIdescMMajorA;
-                    walk([&](int i, int, int valid, int, int) {
-                        const int st = i % p.stages, ph = (i / p.stages) & 1;
-                        if (!mbar_wait(smem_u32(&c->full[st]), ph, abort) || !mbar_wait(smem_u32(&c->made[st]), ph, abort)) return false;
-                        tc_fence_after();
-                        const uint32_t at = ring + st * stage_bytes;
-                        const uint64_t ad = umma_desc_m128(at), bd = umma_desc_k128(at + kRgTile);
-                        for (int k = 0; k * 16 < valid; ++k)
-                            umma_bf16(tmem, ad + (uint64_t)(k * (2048 >> 4)), bd + (uint64_t)(k * 2), idesc, (i > 0 || k > 0) ? 1u : 0u);
-                        umma_commit(smem_u32(&c->empty[st]));
-                        return true;
-                    });
-                }
-            } else {
-                const int wt = tid - 64;
-                const bool e4m3 = p.format == kE4m3;
-                const uint32_t* scales = p.scales + (size_t)(c0 >> 7) * p.T;
-                walk([&](int i, int row0, int valid, int, int) {
-                    const int st = i % p.stages;
-                    const uint32_t at = ring + st * stage_bytes;
-                    uint32_t word[2];
-                    if (raw) {
-#pragma unroll
-                        for (int q = 0; q < 2; ++q) {
-                            const int row = q * 32 + (wt >> 2);
-                            word[q] = row < valid ? ld_after_wait(scales + row0 + row) : 0u;
-                        }
-                    }
-                    if (!mbar_wait_warp(smem_u32(&c->full[st]), (i / p.stages) & 1, abort)) return false;
-                    __syncwarp();
-                    if (raw) {
-                        const int ch = wt & 3;
-#pragma unroll
-                        for (int h = 0; h < 2; ++h)
-#pragma unroll
-                            for (int q = 0; q < 2; ++q) {
-                                const int row = q * 32 + (wt >> 2);
-                                convert16(at + kRgTile + low_bytes + h * (kRgRaw / 2) + row * 64 + ch * 16, at + h * (kRgTile / 2) + row * 128, row, ch,
-                                          scale_of_byte((word[q] >> (8 * (h * 2 + (ch >> 1)))) & 0xffu), e4m3, row < valid);
-                            }
-                        fence_proxy_async_smem();
-                    } else if (valid & 15) {
-                        // rows behind the segment's end that share a step of 16 with its last ones: another token's values times
-                        // zero would be NaN where they are not finite
-                        const int rows = 16 - (valid & 15);
-                        for (int e = wt; e < rows * 16; e += 128) {
-                            const int row = valid + (e >> 4);
-                            st_smem_v4(at + ((e >> 3) & 1) * (kRgTile / 2) + row * 128 + (e & 7) * 16, make_uint4(0, 0, 0, 0));
-                        }
-                        fence_proxy_async_smem();
-                    }
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(smem_u32(&c->made[st]));
-                    return true;
-                });
-            }
-            int base = unit;
-            for (int e = 0; e < total; ++e) {   // where everybody stands after this list
-                const int units = (c->len[e] + 63) / 64;
-                int k = rank - base % S;
-                if (k < 0) k += S;
-                if (k < units) it += (units - k + S - 1) / S;
-                base += units;
-            }
-            unit = base;
-            __syncwarp();
-            __syncthreads();   // (the list is written anew)
-        }
-        if (warp == 1 && it > 0 && !*abort) {
-            if (elect_one()) umma_commit(smem_u32(&c->done));
-        }
-        __syncwarp();
-        bool ok = true;
-        if (warp >= 2 && it > 0) {
-            ok = mbar_wait_warp(smem_u32(&c->done), 0, abort);
-            if (!ok) __nanosleep(50000);
-            __syncwarp();
-            tc_fence_after();
-        }
-        // partial sums: dA [j][column], dB [column][j]
-        const int pitch = job == 0 ? 128 : r16 + 4;
-        if (warp >= 2) {
-            const int row = (warp & 3) * 32 + lane;
-            const uint32_t from = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-            for (int j = 0; j < r16; j += 16) {
-                uint32_t hi[16], lo[16];
-                tmem_ld_32x16(from + (uint32_t)j, hi);
-                tmem_ld_32x16(from + (uint32_t)(r16 + j), lo);
-                tmem_ld_wait();
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const float v = it > 0 && ok ? __uint_as_float(hi[e]) + __uint_as_float(lo[e]) : 0.f;
-                    st_smem_f32(ring + (uint32_t)((job == 0 ? (j + e) * pitch + row : row * pitch + j + e) * 4), v);
-                }
-            }
-            tc_fence_before();
-        }
-        cluster_sync_all();
-        const int d = p.d[job], per = job == 0 ? 32 : r16 / 4;   // float4 per row of the partial sums
-        float* out = p.out[job] + (size_t)slot * kRankPad * d;
-        for (int e = rank * kRgThreads + tid; e < (job == 0 ? r16 : 128) * per; e += S * kRgThreads) {
-            const int row = e / per, col = (e % per) * 4;
-            const int j = job == 0 ? row : col, n = c0 + (job == 0 ? col : row);
-            if (j >= r || n >= d) continue;
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int q = 0; q < S; ++q) {
-                const float4 w = ld_peer_v4(mapa_shared(ring + (uint32_t)((row * pitch + col) * 4), (uint32_t)q));
-                v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
-            }
-            float* dst = job == 0 ? out + (size_t)j * d + n : out + (size_t)n * kRankPad + j;
-            if (job == 0 || j + 4 <= r) {   // (d is a multiple of 8)
-                if (p.accumulate) {
-                    const float4 o = *reinterpret_cast<const float4*>(dst);
-                    v = make_float4(o.x + v.x, o.y + v.y, o.z + v.z, o.w + v.w);
-                }
-                *reinterpret_cast<float4*>(dst) = v;
-            } else {
-                const float w[4] = {v.x, v.y, v.z, v.w};
-                for (int i = 0; j + i < r; ++i) dst[i] = p.accumulate ? dst[i] + w[i] : w[i];
-            }
-        }
-        if (tid == 0 && *abort) atomicOr(p.status[0], LML_FLAG_TIMEOUT);
-        cluster_sync_all();
+    if (mine) {
+        atomicOr(&c->used, 1ull << seg.s);
+        atomicAdd(&c->units[seg.s], mine_units);
     }
     __syncthreads();
+    int pos = 0, before = 0, same = 0;
+    for (int g = 0; g < p.G; ++g) {
+        const int s = c->slot[0][g];
+        if (s < seg.s || (s == seg.s && g < tid)) ++pos;
+        if (s == seg.s && g < tid) { before += c->len[g]; ++same; }
+    }
+    __syncthreads();
+    if (mine) {
+        c->first[pos] = seg.s0; c->len[pos] = seg.s1 - seg.s0; c->piece[pos] = seg.s0 / kTileM + tid; c->pre[pos] = before;
+        if (same == 0) c->entry[seg.s] = pos;
+    }
+    __syncthreads();
+    int total = 0;
+    for (unsigned long long m = c->used; m; m &= m - 1ull) total += p.whole_items ? 1 : c->units[__ffsll((long long)m) - 1];
+    const RgLine line(total * p.all_tiles);
+    const int w0 = p.whole_items ? (int)blockIdx.x : line.begin((int)blockIdx.x), w1 = p.whole_items ? line.W : line.begin((int)blockIdx.x + 1);
+
+    const RgRing ring(smem, p.ring, (uint32_t)p.r16 * 768u);
+    if (w0 < w1) {
+        if (warp == 0) {
+            if (elect_one()) {
+                RgCursor u(ring);
+                const uint32_t* words_end = p.scales + (size_t)kept_groups(p.d[0]) * p.T;
+                for (GradTasks t(p, c, w0, w1); t.next();) {
+                    const int job = t.job(), c0 = t.column(), r16 = chunks_of_rank(p.snap[0].rank[t.slot]) * kChunk, end = t.last() ? kRgLast | kRgEnd : kRgLast;
+                    const bool raw = FMT != kBf16 && job == 0;
+                    const uint32_t* words = p.scales + (size_t)(c0 >> 7) * p.T;
+                    const CUtensorMap* map = &p.map[job];
+                    int flags = kRgFirst;
+                    for (RgPieces v(c, t); v.next(); u.advance()) {
+                        const int row = v.row(), valid = v.valid();
+                        if (v.left == 0) flags |= end;
+                        if (!mbar_wait(smem_u32(&c->empty[u.stage]), u.phase ^ 1u, abort)) break;
+                        const bool touched = raw || (valid & 15);
+                        load_tile(c, map, u.at, u.stage, raw, row, c0, valid, touched ? flags | kRgTouched : flags, r16, words + row, words_end);
+                        if (touched) { post_turn(c, u.turn, u.stage, u.phase); ++u.turn; }
+                        flags = 0;
+                    }
+                }
+                for (int k = 0; k < 2; ++k) post_turn(c, u.turn + k, -1, 0);
+            }
+        } else if (warp == kRgOther) {
+            if (elect_one()) {
+                grid_dependency_wait();   // (the tiles are on their way meanwhile)
+                fence_proxy_async_all();
+                RgCursor u(ring);
+                for (GradTasks t(p, c, w0, w1); t.next();) {
+                    const uint32_t low = (uint32_t)(chunks_of_rank(p.snap[0].rank[t.slot]) * kChunk) * 768u;
+                    const uint8_t* pieces = p.pieces[t.job() ^ 1];   // (u for dy, v for x)
+                    for (RgPieces v(c, t); v.next(); u.advance()) {
+                        if (!mbar_wait(smem_u32(&c->empty[u.stage]), u.phase ^ 1u, abort)) break;
+                        const uint32_t bar = smem_u32(&c->full[u.stage]);
+                        mbar_arrive_expect_tx(bar, low);
+                        bulk_load(u.at + kRgTile, pieces + v.at(), low, bar);
+                    }
+                }
+            }
+        } else if (warp == 1) {
+            if (elect_one()) issue_steps<true>(c, ring, tmem, 3u * (uint32_t)p.r16, abort);
+        } else if (warp < kRgOther) {
+            const int wt = tid - 64;   // (see rows_shrink_kernel)
+            uint32_t items = 0;
+            for (GradTasks t(p, c, w0, w1); t.next(); ++items) {
+                mbar_wait_warp(smem_u32(&c->acc_full[items & 1]), (items >> 1) & 1, abort);
+                __syncwarp();
+                tc_fence_after();
+                // The sums: lane = column.  Partial results: dA [j][column], dB [column][j].
+                const int job = t.job(), c0 = t.column();
+                const int r = p.snap[0].rank[t.slot], r16 = chunks_of_rank(r) * kChunk, row = (warp & 3) * 32 + lane, d = p.d[job];
+                const bool whole = t.whole();
+                float* dst;   // where (column, j) goes: to a partial result every one of them, to the gradients those that there are
+                int stride = 1;   // between two j
+                if (!whole) {
+                    dst = p.partial + (size_t)(2 * blockIdx.x + (line.part_of(t.item()) == (int)blockIdx.x ? 1 : 0)) * kRgPartial + (job == 0 ? row : row * r16);
+                    if (job == 0) stride = 128;
+                } else if (job == 0) {
+                    dst = p.out[0] + (size_t)t.slot * kRankPad * d + c0 + row;
+                    stride = d;
+                } else {
+                    dst = p.out[1] + ((size_t)t.slot * d + c0 + row) * kRankPad;
+                }
+                const uint32_t from = tmem + (items & 1) * 3u * (uint32_t)p.r16 + ((uint32_t)((warp & 3) * 32) << 16);
+                const bool there = !whole || c0 + row < d, add = whole && p.accumulate;
+                const int most = whole ? r : r16;
+#pragma unroll 1
+                for (int j = 0; j < r16; j += 4) {
+                    uint32_t h[4], m[4], l[4];
+                    tmem_ld_32x4(from + (uint32_t)j, h);
+                    tmem_ld_32x4(from + (uint32_t)(r16 + j), m);
+                    tmem_ld_32x4(from + (uint32_t)(2 * r16 + j), l);
+                    tmem_ld_wait();
+                    float s[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[e] = __uint_as_float(h[e]) + (__uint_as_float(m[e]) + __uint_as_float(l[e]));
+                    if (there && job == 1 && j + 4 <= most && !add) {
+                        *reinterpret_cast<float4*>(dst) = make_float4(s[0], s[1], s[2], s[3]);
+                        dst += 4;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e, dst += stride)
+                            if (there && j + e < most) *dst = add ? *dst + s[e] : s[e];
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&c->acc_free[items & 1]));
+                if (whole) continue;
+                const RgShare share = share_of(line, t.item(), t.units, (int)blockIdx.x);
+                if (arrive_last(c, p, share)) {
+                    const int per = job == 0 ? 32 : r16 / 4;   // float4 per row of the partial results
+                    float* out = p.out[job] + (size_t)t.slot * kRankPad * d;
+                    for (int e = wt; e < r16 * 32; e += 32 * kRgFinish) {
+                        const int line_at = e / per, col = (e % per) * 4;
+                        const int j = job == 0 ? line_at : col, n = c0 + (job == 0 ? col : line_at);
+                        if (j >= r || n >= d) continue;
+                        const float4 s = join(p, share, e * 4);
+                        float* dst = job == 0 ? out + (size_t)j * d + n : out + (size_t)n * kRankPad + j;
+                        if (job == 0 || j + 4 <= r) {   // (d is a multiple of 8)
+                            const float4 o = p.accumulate ? *reinterpret_cast<const float4*>(dst) : make_float4(0.f, 0.f, 0.f, 0.f);
+                            *reinterpret_cast<float4*>(dst) = make_float4(o.x + s.x, o.y + s.y, o.z + s.z, o.w + s.w);
+                        } else {
+                            const float w[3] = {s.x, s.y, s.z};   // (less than four columns)
+#pragma unroll
+                            for (int i = 0; i < 3; ++i)
+                                if (j + i < r) dst[i] = p.accumulate ? dst[i] + w[i] : w[i];
+                        }
+                    }
+                }
+            }
+        } else {
+            const int group = (warp - kRgFirstConv) / kRgGroup;
+            convert_tiles<FMT == kE4m3>(c, ring, group, tid - 32 * (kRgFirstConv + group * kRgGroup), lane, abort);
+        }
+    }
+    __syncwarp();
+    if (*abort) __nanosleep(50000);
+    grid_dependency_wait();   // (a CTA without units too: who waits for this grid has waited for the pieces' writers)
+    __syncthreads();
+    if (!p.accumulate) {      // adapters without a token
+        for (unsigned long long m = p.live & ~c->used; m; m &= m - 1ull) {
+            const int slot = __ffsll((long long)m) - 1, r = p.snap[0].rank[slot];
+            const size_t k = (size_t)blockIdx.x * kRgThreads + tid, stride = (size_t)gridDim.x * kRgThreads;
+            for (size_t i = k; i < (size_t)r * p.d[0]; i += stride) p.out[0][(size_t)slot * kRankPad * p.d[0] + i] = 0.f;
+            for (size_t i = k; i < (size_t)r * p.d[1]; i += stride) p.out[1][((size_t)slot * p.d[1] + i / r) * kRankPad + i % r] = 0.f;
+        }
+    }
+    if (tid == 0 && *abort) atomicOr(p.status[0], LML_FLAG_TIMEOUT);
     if (warp == 1) {
         tc_fence_after();
         tmem_dealloc(tmem, cols);
     }
 }
 
+// Calls of several slices: whether their arrays hold together, before any of them adds something.
+__global__ void __launch_bounds__(1024) rows_check_kernel(const int32_t* seg_offsets, int G, int T, int* bad_out)
+{
+    grid_dependency_wait();
+    grid_launch_dependents();
+    int bad = 0;
+    for (int g = threadIdx.x; g < G; g += 1024) {
+        const int s0 = ld_after_wait(seg_offsets + g), s1 = ld_after_wait(seg_offsets + g + 1);
+        if (s1 < s0 || s0 < 0 || s1 > T || (g == 0 && s0 != 0) || (g == G - 1 && s1 != T)) bad = 1;
+    }
+    bad = __syncthreads_or(bad);
+    if (threadIdx.x == 0) *bad_out = bad;
+}
+
 // ---- host ---------------------------------------------------------------------------------------------
-size_t rows_grad_ws_bytes(int T, int G) { return 2 * ((size_t)T / kTileM + (size_t)G) * kRgPiece; }
+constexpr int kRgRing = 208 * 1024;   // one CTA to an SM
 
-constexpr int kRgSmemMax = 1024 + 108 * 1024;   // two CTAs to an SM
+// Workspace: [u][v][partial results of both passes' CTAs][whether the arrays hold together]
+struct RgLayout { size_t pieces, partial, bad, total; };
+static RgLayout rg_layout(int T, int G, int num_sms)
+{
+    RgLayout l;
+    l.pieces = ((size_t)T / kTileM + (size_t)(G < kRgSegs ? G : kRgSegs)) * kRgPiece;
+    l.partial = 2 * l.pieces;
+    l.bad = l.partial + (size_t)num_sms * 2 * kRgPartial * sizeof(float);
+    l.total = l.bad + 256;
+    return l;
+}
+size_t rows_grad_ws_bytes(int T, int G, int num_sms) { return rg_layout(T, G, num_sms).total; }
 
+template <int FMT> static cudaError_t rg_attributes()
+{
+    cudaError_t e = cudaFuncSetAttribute(rows_shrink_kernel<FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, 1024 + kRgRing);
+    if (e != cudaSuccess) return e;
+    return cudaFuncSetAttribute(rows_grad_kernel<FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, 1024 + kRgRing);
+}
 cudaError_t rows_grad_init()
 {
-    cudaError_t e = cudaFuncSetAttribute(rows_shrink_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRgSmemMax);
-    if (e != cudaSuccess) return e;
-    return cudaFuncSetAttribute(rows_grad_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRgSmemMax);
+    cudaError_t e = rg_attributes<kBf16>();
+    if (e == cudaSuccess) e = rg_attributes<kInt8>();
+    if (e == cudaSuccess) e = rg_attributes<kE4m3>();
+    return e;
 }
 
 cudaError_t launch_rows_grad(const RowsGradCall& a, cudaStream_t stream, int* launches)
@@ -570,58 +909,72 @@ cudaError_t launch_rows_grad(const RowsGradCall& a, cudaStream_t stream, int* la
             p.live |= 1ull << s;
             ++live;
         }
-    if (live == 0) most = 1;
+    if (live == 0) return cudaSuccess;
     p.r16 = chunks_of_rank(most) * kChunk;
+    const RgLayout lay = rg_layout(a.T, a.G, a.num_sms);
+    uint8_t* ws = static_cast<uint8_t*>(a.workspace);
     p.d[0] = a.d_in; p.d[1] = a.d_out;
-    p.T = a.T; p.G = a.G; p.format = a.x.format; p.accumulate = a.accumulate ? 1 : 0;
+    p.tiles[0] = (a.d_in + 127) / 128; p.tiles[1] = (a.d_out + 127) / 128;
+    p.all_tiles = p.tiles[0] + p.tiles[1];
+    p.T = a.T; p.ring = kRgRing;
     p.scales = a.x.scales;
-    p.seg_offsets = a.seg_offsets; p.ids = a.ids; p.ids_T = a.ids_T;
     p.status[0] = a.status; p.status[1] = a.status_T;
-    const size_t blocks = (size_t)a.T / kTileM + (size_t)a.G;
-    p.pieces[0] = static_cast<uint8_t*>(a.workspace);
-    p.pieces[1] = p.pieces[0] + blocks * kRgPiece;
+    p.pieces[0] = ws; p.pieces[1] = ws + lay.pieces;
+    p.partial = reinterpret_cast<float*>(ws + lay.partial);
+    p.arrived = a.arrived;
     p.out[0] = a.dA; p.out[1] = a.dB;
-    p.tiles0 = (a.d_in + 127) / 128;
-    const int tiles = p.tiles0 + (a.d_out + 127) / 128;
-    p.low[0] = *a.tmap_A; p.low[1] = *a.tmap_AT;
-    if (a.T > 0) {
-        const int pitch = kept_pitch(a.d_in);
-        const bool ok = a.x.format == kBf16 ? a.cache->get_2d(&p.map[0], a.x.data, (uint64_t)a.d_in, (uint64_t)a.T, (uint64_t)a.d_in * 2, 64, 64)
-                                            : a.cache->get_2d(&p.map[0], a.x.data, (uint64_t)pitch / 2, (uint64_t)a.T, (uint64_t)pitch, 32, 64, false);
-        if (!ok || !a.cache->get_2d(&p.map[1], a.dy, (uint64_t)a.d_out, (uint64_t)a.T, (uint64_t)a.d_out * 2, 64, 64)) return cudaErrorInvalidValue;
-    } else {
-        memset(p.map, 0, sizeof(p.map));
-    }
-    const int raw = a.x.format != kBf16 ? kRgRaw : 0;
-    auto config = [&](cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&attr)[2], dim3 grid, int stage) {
-        p.stages = (kRgSmemMax - 1024) / stage;
-        if (p.stages > kRgMaxStages) p.stages = kRgMaxStages;
-        pdl_config(cfg, attr, grid, dim3(kRgThreads), (size_t)(1024 + p.stages * stage), stream);
-        attr[1].id = cudaLaunchAttributeClusterDimension;
-        attr[1].val.clusterDim.x = (unsigned)p.S;
-        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-        cfg.numAttrs = 2;
+    memset(p.map, 0, sizeof(p.map));
+    memset(p.low, 0, sizeof(p.low));
+    auto launch = [&](void (*kernel)(RowsGradParams), long long ctas) {
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute attr[1];
+        const long long all = a.num_sms;
+        pdl_config(cfg, attr, dim3((unsigned)(ctas < 1 ? 1 : ctas < all ? ctas : all)), dim3(kRgThreads), (size_t)(1024 + kRgRing), stream);
+        const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p);
+        if (e == cudaSuccess) ++*launches;
+        return e;
     };
-    cudaLaunchConfig_t cfg;
-    cudaLaunchAttribute attr[2];
-    if (a.T > 0 && live > 0) {
-        cfg = {};
-        p.S = 8;
-        while (p.S > 2 && (long long)blocks * 2 * p.S > 8ll * a.num_sms) p.S >>= 1;
-        config(cfg, attr, dim3((unsigned)(blocks * p.S), 2), kRgTile + p.r16 * 128 + raw);
-        const cudaError_t e = cudaLaunchKernelEx(&cfg, rows_shrink_kernel, p);
+    const bool e4m3 = a.x.format == kE4m3, bf16 = a.x.format == kBf16;
+    const auto shrink = bf16 ? rows_shrink_kernel<kBf16> : e4m3 ? rows_shrink_kernel<kE4m3> : rows_shrink_kernel<kInt8>;
+    const auto grad = bf16 ? rows_grad_kernel<kBf16> : e4m3 ? rows_grad_kernel<kE4m3> : rows_grad_kernel<kInt8>;
+    p.bad = nullptr;
+    if (a.T == 0) {   // adapters' gradients are zero
+        p.G = 0; p.seg_offsets = p.ids = p.ids_T = nullptr;
+        p.check_first = p.check_last = 0; p.accumulate = 0; p.whole_items = 0;
+        return launch(grad, a.num_sms);
+    }
+    const int pitch = kept_pitch(a.d_in);
+    bool ok = bf16 ? a.cache->get_2d(&p.map[0], a.x.data, (uint64_t)a.d_in, (uint64_t)a.T, (uint64_t)a.d_in * 2, 64, kTileM)
+                   : a.cache->get_2d(&p.map[0], a.x.data, (uint64_t)pitch / 2, (uint64_t)a.T, (uint64_t)pitch, 64, kTileM, false);   // (8-bit rows as pairs)
+    ok = ok && a.cache->get_2d(&p.map[1], a.dy, (uint64_t)a.d_out, (uint64_t)a.T, (uint64_t)a.d_out * 2, 64, kTileM);
+    for (int k = 0; k < kRankPad / kChunk && k * kChunk < p.r16; ++k)
+        for (int i = 0; i < 2; ++i)
+            ok = ok && a.cache->get_2d(&p.low[i][k], a.low[i], (uint64_t)p.d[i], (uint64_t)a.slots[i] * kRankPad, (uint64_t)p.d[i] * 2, 64, (k + 1) * kChunk);
+    if (!ok) return cudaErrorInvalidValue;
+    if (a.G > kRgSegs) {
+        p.bad = reinterpret_cast<int*>(ws + lay.bad);
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute attr[1];
+        pdl_config(cfg, attr, dim3(1), dim3(1024), 0, stream);
+        const cudaError_t e = cudaLaunchKernelEx(&cfg, rows_check_kernel, a.seg_offsets, a.G, a.T, const_cast<int*>(p.bad));
         if (e != cudaSuccess) return e;
         ++*launches;
     }
-    const int z = !a.accumulate ? live : (a.G < live ? a.G : live);
-    if (z > 0 && (a.T > 0 || !a.accumulate)) {
-        cfg = {};
-        p.S = 8;
-        while (p.S > 1 && ((a.T + 63) / 64 < p.S || (long long)tiles * z * p.S > 8ll * a.num_sms)) p.S >>= 1;
-        config(cfg, attr, dim3((unsigned)(tiles * p.S), (unsigned)z), kRgTile + p.r16 * 256 + raw);
-        const cudaError_t e = cudaLaunchKernelEx(&cfg, rows_grad_kernel, p);
+    for (int g0 = 0; g0 < a.G; g0 += kRgSegs) {
+        p.G = a.G - g0 < kRgSegs ? a.G - g0 : kRgSegs;
+        p.seg_offsets = a.seg_offsets + g0; p.ids = a.ids + g0; p.ids_T = a.ids_T + g0;
+        p.check_first = g0 == 0; p.check_last = g0 + p.G == a.G;
+        p.accumulate = a.accumulate || g0 > 0 ? 1 : 0;
+        p.whole_items = 0;
+        const long long pieces = (a.T + kTileM - 1) / kTileM;
+        cudaError_t e = launch(shrink, pieces * p.all_tiles / kRgLeast);
         if (e != cudaSuccess) return e;
-        ++*launches;
+        // Few pieces to an item: whole items, unless there are so many that their number leaves CTAs idle at the end.
+        const int slots = p.G < live ? p.G : live;
+        const long long items = (long long)p.all_tiles * slots;
+        p.whole_items = pieces <= 4ll * slots && items <= a.num_sms;
+        e = launch(grad, p.whole_items ? items : pieces * p.all_tiles / kRgLeast);
+        if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
 }

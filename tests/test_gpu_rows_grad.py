@@ -251,6 +251,24 @@ def test_captured_and_on_a_stream_of_its_own():
     c.close()
 
 
+@pytest.mark.parametrize("form", ("int8", "bf16"))
+def test_many_calls_back_to_back(form):
+    """Long runs of whole units beside short ones, call after call without a pause: no role of a kernel may fall a turn of its ring behind."""
+    import torch
+    c = Case(1500, 1032, 4104, [16, 33], [900, 7, 593], [0, 1, 1])
+    x, dy = c.rows(form), to_dev(c.dy)
+    want = c.run(form)
+    sets = [c.buffers() for _ in range(3)]
+    for k in range(30):
+        _, _, dA, dB = sets[k % 3]
+        c.t.backward_adapters_rows(c.tT, x, dy, c.so, c.ids, c.ids_T, dA, dB, accumulate=False)
+    torch.cuda.synchronize()
+    for _, _, dA, dB in sets:
+        assert np.array_equal(dA.cpu().numpy(), want[0]) and np.array_equal(dB.cpu().numpy(), want[1])
+    c.check(*want, form)
+    c.close()
+
+
 def test_near_the_call_that_rounds_its_small_products():
     """lora_mixed_linear_backward_adapters on the same bf16 rows: its rounding of u and v, 2^-9 of every term, and no more."""
     import torch
