@@ -419,23 +419,47 @@ def _stream(stream) -> int:
     return int(_current_raw_stream())
 
 
-def _stream_on(device, stream) -> int:
+_raw_stream_of = None
+_bf16 = None
+
+
+def _stream_on(device: int, stream) -> int:
     """The given stream, or the current one of the tensors' device (which need not be the current device)."""
     if stream is not None:
         return int(stream.cuda_stream)
-    import torch
-    if device.index == torch.cuda.current_device():
-        return _stream(None)
-    return int(torch.cuda.current_stream(device).cuda_stream)
+    global _raw_stream_of
+    if _raw_stream_of is None:
+        import torch
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        _raw_stream_of = raw if raw is not None else (lambda d: torch.cuda.current_stream(d).cuda_stream)
+    return _raw_stream_of(device)
 
 
-def _bf16_rows(t, T, d, name, device=None):
-    """Checks a bf16 [T][d] tensor of the call; None passes."""
+def _bf16_rows(t, shape, name, device: int) -> int:
+    """Checks a bf16 [T][d] tensor of a call on cuda:`device` and gives its address; None is 0."""
+    if t is None:
+        return 0
+    global _bf16
+    if _bf16 is None:
+        import torch
+        _bf16 = torch.bfloat16
+    assert t.dtype is _bf16 and t.shape == shape and t.is_contiguous(), (name, t.shape, t.dtype)
+    assert t.get_device() == device, (name, t.device)
+    return t.data_ptr()
+
+
+def _sums(t, d, name, device: int) -> int:
+    """Checks a float32 [d] tensor that a call adds to, and gives its address; None is 0."""
+    if t is None:
+        return 0
     import torch
-    if t is not None:
-        assert t.dtype == torch.bfloat16 and t.is_cuda and t.is_contiguous() and tuple(t.shape) == (T, d), (name, t.shape, t.dtype)
-        assert device is None or t.device == device, (name, t.device)
-    return t
+    assert t.dtype is torch.float32 and t.shape == (d,) and t.is_contiguous() and t.get_device() == device, (name, t.shape, t.dtype)
+    return t.data_ptr()
+
+
+def _cuda_index(t, name) -> int:
+    assert t.is_cuda, name
+    return t.get_device()
 
 
 class Checkpoint:
@@ -446,11 +470,12 @@ class Checkpoint:
         import torch
         T = int(data.shape[0])
         assert form in ("int8", "e4m3"), form
-        assert data.dtype == torch.uint8 and scales.dtype == torch.uint8 and data.is_cuda and scales.device == data.device
+        self.device = _cuda_index(data, "data")
+        assert data.dtype is torch.uint8 and scales.dtype is torch.uint8 and scales.get_device() == self.device
         assert data.is_contiguous() and scales.is_contiguous() and width > 0 and width % 8 == 0
-        assert tuple(data.shape) == (T, (width + 31) // 32 * 32) and tuple(scales.shape) == ((width + 127) // 128, T, 4), (data.shape, scales.shape)
+        assert data.shape == (T, (width + 31) // 32 * 32) and scales.shape == ((width + 127) // 128, T, 4), (data.shape, scales.shape)
         self.data, self.scales, self.tokens, self.width, self.form = data, scales, T, int(width), form
-        self.rows = Rows(_ptr(data), _ptr(scales), ROW_FORMS[form])
+        self.rows = Rows(data.data_ptr(), scales.data_ptr(), ROW_FORMS[form])
 
     @classmethod
     def empty(cls, tokens: int, width: int, form: str, device="cuda") -> "Checkpoint":
@@ -463,18 +488,17 @@ class Checkpoint:
 
     def store(self, x, stream=None) -> "Checkpoint":
         """Keep x (bf16 [tokens][width])."""
-        _bf16_rows(x, self.tokens, self.width, "x", self.data.device)
-        lml_checkpoint_store(x.device.index, _ptr(x), self.tokens, self.width, self.rows, _stream_on(x.device, stream))
+        lml_checkpoint_store(self.device, _bf16_rows(x, (self.tokens, self.width), "x", self.device), self.tokens, self.width, self.rows,
+                             _stream_on(self.device, stream))
         return self
 
     def load(self, out=None, stream=None):
         """The values it stands for, bf16 [tokens][width]."""
         import torch
-        dev = self.data.device
+        shape, dev = (self.tokens, self.width), self.device
         if out is None:
-            out = torch.empty((self.tokens, self.width), dtype=torch.bfloat16, device=dev)
-        _bf16_rows(out, self.tokens, self.width, "out", dev)
-        lml_checkpoint_load(dev.index, self.rows, self.tokens, self.width, _ptr(out), _stream_on(dev, stream))
+            out = torch.empty(shape, dtype=torch.bfloat16, device=self.data.device)
+        lml_checkpoint_load(dev, self.rows, self.tokens, self.width, _bf16_rows(out, shape, "out", dev), _stream_on(dev, stream))
         return out
 
 
@@ -483,15 +507,14 @@ def checkpoint_store(x, form: str = "int8", stream=None) -> Checkpoint:
     return Checkpoint.empty(int(x.shape[0]), int(x.shape[1]), form, x.device).store(x, stream)
 
 
-def _as_rows(x, T, d, name, device):
+def _as_rows(x, shape, name, device: int):
     """Rows of a call: a bf16 tensor or a Checkpoint."""
     if x is None:
         return None
     if isinstance(x, Checkpoint):
-        assert x.tokens == T and x.width == d and x.data.device == device, (name, x.tokens, x.width)
+        assert (x.tokens, x.width) == shape and x.device == device, (name, x.tokens, x.width)
         return x.rows
-    _bf16_rows(x, T, d, name, device)
-    return Rows(_ptr(x), None, ROWS_BF16)
+    return Rows(_bf16_rows(x, shape, name, device), None, ROWS_BF16)
 
 
 class BlockNorm:
@@ -505,24 +528,25 @@ class BlockNorm:
         for name, w in (("w_post", w_post), ("w_pre", w_pre), ("gate", gate)):
             assert w is None or (w.dtype == torch.bfloat16 and w.is_cuda and w.is_contiguous() and tuple(w.shape) == (d,)), name
         self.d, self.w_post, self.w_pre, self.gate, self.scale, self.eps = d, w_post, w_pre, gate, float(scale), float(eps)
-        self.device = next((w.device for w in (w_post, w_pre, gate) if w is not None), None)
+        self.device = next((w.get_device() for w in (w_post, w_pre, gate) if w is not None), None)
+        assert all(w is None or w.get_device() == self.device for w in (w_post, w_pre, gate)), "weights on several devices"
         self.desc = BlockNormDesc(d, eps, scale, _ptr(w_post), _ptr(w_pre), _ptr(gate))
 
     def forward(self, h, o=None, gate_rows=None, h_new=None, x=None, x_checkpoint=None, h_checkpoint=None, stream=None):
         """-> (h', x).  o None: h' is h.  gate_rows: a gate per token, bf16 [T][d].  h_new / x: where to write them (new tensors otherwise);
         x_checkpoint / h_checkpoint: Checkpoints that the same pass fills.  x is None without w_pre."""
         import torch
-        T, d, dev = int(h.shape[0]), self.d, h.device
+        T, dev = int(h.shape[0]), _cuda_index(h, "h")
+        shape = (T, self.d)
         assert self.device is None or dev == self.device, dev
-        for name, t in (("h", h), ("o", o), ("gate_rows", gate_rows), ("h_new", h_new), ("x", x)):
-            _bf16_rows(t, T, d, name, dev)
+        h_at = _bf16_rows(h, shape, "h", dev)
         if h_new is None and o is not None:
             h_new = torch.empty_like(h)
         if x is None and self.w_pre is not None:
             x = torch.empty_like(h)
-        lml_block_norm(dev.index, self.desc, T, _ptr(h), _ptr(o), _ptr(gate_rows), _ptr(h_new), _ptr(x),
-                       _as_rows(x_checkpoint, T, d, "x_checkpoint", dev), _as_rows(h_checkpoint, T, d, "h_checkpoint", dev),
-                       _stream_on(dev, stream))
+        lml_block_norm(dev, self.desc, T, h_at, _bf16_rows(o, shape, "o", dev), _bf16_rows(gate_rows, shape, "gate_rows", dev),
+                       _bf16_rows(h_new, shape, "h_new", dev), _bf16_rows(x, shape, "x", dev), _as_rows(x_checkpoint, shape, "x_checkpoint", dev),
+                       _as_rows(h_checkpoint, shape, "h_checkpoint", dev), _stream_on(dev, stream))
         return (h if o is None else h_new), x
 
     def backward(self, h_new, o, dx, dh_new, gate_rows=None, dh=None, d_o=None, dw_pre=None, dw_post=None, dgate=None, workspace=None,
@@ -532,12 +556,11 @@ class BlockNorm:
         gate_rows their gradient, bf16 [T][d]."""
         import torch
         some = dx if dx is not None else dh_new
-        T, d, dev = int(some.shape[0]), self.d, some.device
+        T, d, dev = int(some.shape[0]), self.d, _cuda_index(some, "dx")
+        shape = (T, d)
         assert self.device is None or dev == self.device, dev
-        for name, t in (("dx", dx), ("dh_new", dh_new), ("gate_rows", gate_rows), ("dh", dh), ("d_o", d_o)):
-            _bf16_rows(t, T, d, name, dev)
-        for name, t in (("dw_pre", dw_pre), ("dw_post", dw_post), ("dgate", dgate)):
-            assert t is None or (t.dtype == torch.float32 and t.is_contiguous() and tuple(t.shape) == (d,) and t.device == dev), name
+        dx_at, dh_new_at = _bf16_rows(dx, shape, "dx", dev), _bf16_rows(dh_new, shape, "dh_new", dev)
+        gate_at = _bf16_rows(gate_rows, shape, "gate_rows", dev)
         if dh is None:
             dh = torch.empty_like(some)
         if d_o is None and o is not None:
@@ -545,12 +568,13 @@ class BlockNorm:
         dgate_rows = torch.empty_like(gate_rows) if gate_rows is not None else None
         n_ws = 0
         if dw_pre is not None or dw_post is not None or dgate is not None:
-            n_ws = lml_block_norm_workspace_bytes(dev.index, T, d)
             if workspace is None:
-                workspace = torch.empty(max(n_ws, 256), dtype=torch.uint8, device=dev)
-            n_ws = int(workspace.numel())
-        lml_block_norm_backward(dev.index, self.desc, T, _as_rows(h_new, T, d, "h_new", dev), _as_rows(o, T, d, "o", dev), _ptr(gate_rows),
-                                _ptr(dx), _ptr(dh_new), _ptr(dh), _ptr(d_o), _ptr(dw_pre), _ptr(dw_post), _ptr(dgate), _ptr(dgate_rows),
+                workspace = torch.empty(max(lml_block_norm_workspace_bytes(dev, T, d), 256), dtype=torch.uint8, device=some.device)
+            assert workspace.get_device() == dev, "workspace"
+            n_ws = workspace.numel()
+        lml_block_norm_backward(dev, self.desc, T, _as_rows(h_new, shape, "h_new", dev), _as_rows(o, shape, "o", dev), gate_at, dx_at, dh_new_at,
+                                _bf16_rows(dh, shape, "dh", dev), _bf16_rows(d_o, shape, "d_o", dev), _sums(dw_pre, d, "dw_pre", dev),
+                                _sums(dw_post, d, "dw_post", dev), _sums(dgate, d, "dgate", dev), _ptr(dgate_rows),
                                 _ptr(workspace) if n_ws else 0, n_ws, _stream_on(dev, stream))
         return dh, d_o, (dgate_rows if gate_rows is not None else dgate)
 
@@ -719,17 +743,21 @@ class Table:
         """backward_adapters with x as a Checkpoint (or a bf16 tensor) and unrounded small products.  accumulate=False: the rows j < rank of
         every live slot are written, so that dA and dB need not be zeroed before a step's first batch."""
         import torch
-        T, G, dev = int(dy.shape[0]), int(slot_ids.shape[0]), dy.device
-        assert dA.dtype == torch.float32 and dB.dtype == torch.float32 and dA.is_contiguous() and dB.is_contiguous()
-        assert tuple(dA.shape) == (self.max_slots, 64, self.d_in) and tuple(dB.shape) == (self.max_slots, self.d_out, 64)
-        assert seg_offsets.dtype == slot_ids.dtype == slot_ids_T.dtype == torch.int32
-        assert int(seg_offsets.shape[0]) == G + 1 and int(slot_ids_T.shape[0]) == G
-        _bf16_rows(dy, T, self.d_out, "dy")
+        T, G, dev = int(dy.shape[0]), int(slot_ids.shape[0]), self.device
+        assert dA.dtype is torch.float32 and dB.dtype is torch.float32 and dA.is_contiguous() and dB.is_contiguous()
+        assert dA.shape == (self.max_slots, 64, self.d_in) and dB.shape == (self.max_slots, self.d_out, 64)
+        assert seg_offsets.dtype is slot_ids.dtype is slot_ids_T.dtype is torch.int32
+        assert seg_offsets.shape[0] == G + 1 and slot_ids_T.shape[0] == G
+        assert seg_offsets.is_contiguous() and slot_ids.is_contiguous() and slot_ids_T.is_contiguous()
+        for t in (dA, dB, seg_offsets, slot_ids, slot_ids_T):
+            assert t.get_device() == dev, t.device
+        dy_at = _bf16_rows(dy, (T, self.d_out), "dy", dev)
         if workspace is None:
-            workspace = torch.empty(max(lml_backward_rows_workspace_bytes(self.handle, T, G), 256), dtype=torch.uint8, device=dev)
-        lora_mixed_linear_backward_adapters_rows(self.handle, table_T.handle, _as_rows(x, T, self.d_in, "x", dev), _ptr(dy), T,
-                                                 _ptr(seg_offsets), _ptr(slot_ids), _ptr(slot_ids_T), G, _ptr(dA), _ptr(dB), accumulate,
-                                                 _ptr(workspace), int(workspace.numel()), _stream_on(dev, stream))
+            workspace = torch.empty(max(lml_backward_rows_workspace_bytes(self.handle, T, G), 256), dtype=torch.uint8, device=dy.device)
+        assert workspace.get_device() == dev, "workspace"
+        lora_mixed_linear_backward_adapters_rows(self.handle, table_T.handle, _as_rows(x, (T, self.d_in), "x", dev), dy_at, T,
+                                                 seg_offsets.data_ptr(), slot_ids.data_ptr(), slot_ids_T.data_ptr(), G, dA.data_ptr(),
+                                                 dB.data_ptr(), accumulate, workspace.data_ptr(), workspace.numel(), _stream_on(dev, stream))
 
     def lora_mixed_linear_dual(self, x, W0, seg_offsets, slot_ids_a, slot_ids_b, perm=None, stream=None):
         """-> (y_a, y_b): the layer under two slot bindings of the same segments."""
