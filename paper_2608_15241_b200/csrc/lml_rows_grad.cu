@@ -5,15 +5,18 @@
 // rows_shrink_kernel: u and v.  An item is a piece (up to 128 rows of one segment, counted from the segment's first row: a TMA box
 // may begin at any row, so no row of another segment is in it but behind its end) of x or of dy, its work the steps of 128 columns.
 // rows_grad_kernel: dA and dB.  An item is (slot, 128 columns of x or dy), its work the slot's pieces.
-// A step of either is a tile of 128 rows x 128 columns.
+// A step of either is a tile of 128 rows x 128 columns, which goes through the rings in two halves along what is contracted: 64 columns in the
+// first pass, 64 rows in the second: a stage's way through loading, conversion and product is some 4000 cycles whatever its size, so
+// what counts is how many there are (three stages for the six and four that fit beside 64 ranks: 240 us for 180).
 // In both the work of all items stands in one line that is cut into equal parts, one per SM; a CTA walks its part without a pause
 // between items.  An item that the cuts divide is joined in device memory: every CTA writes its partial result, and the last one to
 // arrive adds them in the order of the parts, so the bits do not depend on who that is.  (A form with a cluster per item and an
 // exchange through distributed shared memory spent 10 us per CTA on setting up and joining.)
 //
-// Both are rings of tiles of x or dy as TMA brings them in, multiplied by tcgen05 into one of two accumulators.  Roles: a producer of tiles,
-// which also tells the others what a stage holds, and one of the other operand (one thread for both would be the slowest role); an issuer; four warps that finish items while the next one is multiplied; two
-// groups of eight warps that take 8-bit tiles in turn through their registers and write them back in place as bf16 (exact: the
+// Both are rings of tiles of x or dy as TMA brings them in, multiplied by tcgen05 into one of two accumulators.  Roles: three producers, of
+// tiles, of the other operand and of scale words (one thread for two of them is the slowest role: a copy costs it a few hundred cycles), the
+// second of which tells the others what a stage holds; an issuer; four warps that finish items while the next one is multiplied;
+// groups of warps that take 8-bit tiles in turn through their registers and write them beside as bf16 (exact: the
 // scales are powers of two) in the swizzled order of the tensor cores.  The second product contracts over tokens: the tile
 // [token][64 columns] is an operand whose contiguous index is the output's (M-major), which the descriptor says; nothing is
 // transposed.
@@ -31,25 +34,26 @@ namespace lml {
 
 using namespace ptx;
 
-constexpr int kRgGroup = 8;                     // warps of a converting group
+constexpr int kRgGroups = 2, kRgGroup = 8;      // converting groups, warps of each
 constexpr int kRgFinish = 4;                    // warps that finish items (warps 2 ... 5: one per quarter of the accumulator's lanes)
 constexpr int kRgOther = 2 + kRgFinish;         // the warp that brings in the other operand
-constexpr int kRgFirstConv = kRgOther + 1;
-constexpr int kRgThreads = 32 * (kRgFirstConv + 2 * kRgGroup);
+constexpr int kRgWordsWarp = kRgOther + 1;      // ... and the scale words
+constexpr int kRgFirstConv = kRgWordsWarp + 1;
+constexpr int kRgThreads = 32 * (kRgFirstConv + kRgGroups * kRgGroup);
 constexpr int kRgSegs = 320;                    // segments of a launch; a call of more runs in slices
-constexpr int kRgTile = 128 * 128 * 2;          // bytes of a tile as it is multiplied: two halves of 64 columns, [half][row][64]
+constexpr int kRgTile = 128 * 64 * 2;           // bytes of half a step as it is multiplied: [row][64 columns], or two times [64 rows][64 columns]
 constexpr int kRgHalfTile = kRgTile / 2;
-constexpr int kRgRaw = 128 * 128;               // ... of the 8-bit tile it is made of, [row][128]
+constexpr int kRgRaw = 128 * 64;                // ... of the 8 bits that it is made of, [128][64] or [64][128]
 constexpr int kRgPiece = 2 * 3 * kRankPad * 128;   // u (or v) of a piece: [64 tokens each][three parts][column][64]
 constexpr int kRgPartial = kRankPad * 128;      // floats of a partial result
-constexpr int kRgMaxStages = 6;
-constexpr int kRgTurns = 16;                    // tiles on their way to and from the converting warps: as many as stages, and two ends
-static_assert(kRgTurns >= kRgMaxStages + 2 && (kRgTurns & (kRgTurns - 1)) == 0, "a turn's place must have been read before it is used again");
-constexpr int kRgWords = 136;                   // scale words of a tile, one per row, brought in from a 16-byte boundary on
+constexpr int kRgMaxStages = 10;
+constexpr int kRgTurns = 16;                    // tiles on their way to and from the converting warps: as many as stages, and an end for each group
+static_assert(kRgTurns >= kRgMaxStages + kRgGroups && (kRgTurns & (kRgTurns - 1)) == 0, "a turn's place must have been read before it is used again");
+constexpr int kRgWords = 136;                   // scale words of half a step, one per row, brought in from a 16-byte boundary on (of 64 rows: 72)
 constexpr int kRgLeast = 4;                     // steps of a CTA's part (of a whole pass, if it has fewer)
 
 struct alignas(64) RowsGradParams {
-    CUtensorMap map[2];       // x, dy: boxes of 64 columns (8-bit x: 128) x 128 rows
+    CUtensorMap map[2][2];    // x, dy; first pass: boxes of 64 columns x 128 rows; second: 64 (8-bit x: 128) x 64
     CUtensorMap low[2][kRankPad / kChunk];   // the packed A of the table, B^T of the transposed one: boxes of 64 columns x 16, 32, 48, 64 rows
     SlotSnapshot snap[2];     // table, transposed table
     const uint32_t* scales;   // of x
@@ -67,7 +71,8 @@ struct alignas(64) RowsGradParams {
 };
 
 // What the producer says about a stage.
-constexpr int kRgFirst = 1, kRgLast = 2, kRgEnd = 4, kRgTouched = 8;   // first, last of an item; last of this CTA; goes through the converting warps
+// first, last of an item; last of this CTA; goes through the converting warps; the right half of 128 columns
+constexpr int kRgFirst = 1, kRgLast = 2, kRgEnd = 4, kRgTouched = 8, kRgRight = 16;
 struct RgInfo {
     int flags, valid;   // rows
     int r16;            // columns of the other operand (second pass: of each of its three parts)
@@ -75,16 +80,24 @@ struct RgInfo {
 };
 struct RgTurn { int stage, phase; };   // stage < 0: no more
 
+// An item that this CTA is to join: all of its threads do, when its part of the line is done.  (Four finishing warps on their own, with two or four
+// loads in flight, took up to 9 us.)
+struct RgJoin { int job, slot, first, last, at, valid; };   // at: piece (first pass), column (second)
+
 struct RgCtrl {
     unsigned long long full[kRgMaxStages], empty[kRgMaxStages], turn[kRgTurns], made[kRgTurns], acc_full[2], acc_free[2];
     RgInfo info[kRgMaxStages];
     RgTurn turns[kRgTurns];
-    unsigned long long used;
+    uint32_t used_half[2];   // slots in use
+    __device__ unsigned long long used() const { return (unsigned long long)used_half[1] << 32 | used_half[0]; }
     uint32_t tmem_base;
-    int abort, last, count[kRgSegs / 32], units[kMaxSlots], entry[kMaxSlots];
+    RgJoin joins[2];   // (a part has at most two items that are not whole)
+    int n_joins;
+    int abort, count[kRgSegs / 32], units[kMaxSlots], entry[kMaxSlots];
     int first[kRgSegs], len[kRgSegs], piece[kRgSegs], pre[kRgSegs + 1];
     uint8_t slot[2][kRgSegs];
     alignas(16) uint32_t words[kRgMaxStages][kRgWords];
+    float4 turned[kRgFinish][32][5];
 };
 
 __device__ __forceinline__ uint64_t umma_desc_m128(uint32_t smem_addr)   // 64 contiguous M per 128-byte swizzled row, rows along K
@@ -99,15 +112,16 @@ __device__ __forceinline__ uint64_t umma_desc_m128(uint32_t smem_addr)   // 64 c
 }
 constexpr uint32_t kIdescMMajorA = 1u << 15;
 
-// 4 columns of 32 lanes
-__device__ __forceinline__ void tmem_ld_32x4(uint32_t taddr, uint32_t (&r)[4])
+// 8 columns of 32 lanes
+__device__ __forceinline__ void tmem_ld_32x8(uint32_t taddr, uint32_t (&r)[8])
 {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr) : "memory");
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr) : "memory");
 }
-__device__ __forceinline__ uint2 ld_smem_v2(uint32_t a)
+__device__ __forceinline__ uint4 ld_smem_v4(uint32_t a)
 {
-    uint2 v;
-    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
     return v;
 }
 __device__ __forceinline__ void st_smem_v4(uint32_t a, const uint4& v)
@@ -121,15 +135,6 @@ __device__ __forceinline__ float4 ld_cg_v4(const float* p)   // (written by anot
     return v;
 }
 __device__ __forceinline__ void finish_barrier() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kRgFinish) : "memory"); }
-// Of a converting group; whether any thread says so.
-__device__ __forceinline__ bool group_any(int group, bool v)
-{
-    int r;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.s32 p, %1, 0;\n\tbar.red.or.pred q, %2, %3, p;\n\tselp.s32 %0, 1, 0, q;\n\t}"
-                 : "=r"(r) : "r"(v ? 1 : 0), "r"(2 + group), "n"(32 * kRgGroup) : "memory");
-    return r != 0;
-}
-
 // Whether a segment's two bindings name one adapter in both tables.
 __device__ __forceinline__ bool paired(const RowsGradParams& p, int s, int sT)
 {
@@ -141,9 +146,10 @@ __device__ __forceinline__ void rg_setup(RgCtrl* c, int warp, int tid, uint32_t 
 {
     if (tid == 0) {
         c->abort = 0;
-        c->used = 0ull;
+        c->n_joins = 0;
+        c->used_half[0] = c->used_half[1] = 0u;
         for (int i = 0; i < kRgMaxStages; ++i) {
-            mbar_init(smem_u32(&c->full[i]), 2);
+            mbar_init(smem_u32(&c->full[i]), 3);
             mbar_init(smem_u32(&c->empty[i]), 1);
         }
         for (int i = 0; i < kRgTurns; ++i) {
@@ -163,12 +169,16 @@ __device__ __forceinline__ void rg_setup(RgCtrl* c, int warp, int tid, uint32_t 
 }
 __device__ __forceinline__ uint32_t tmem_cols_for(int n) { return n <= 32 ? 32u : n <= 64 ? 64u : n <= 128 ? 128u : n <= 256 ? 256u : 512u; }
 
-// The ring of a CTA: stages of a tile beside the other operand (of the widest adapter).  Every role walks it with a cursor of its own (a
-// division per step to find the stage costs as much as the step's products).
+// The ring of a CTA: stages of a tile as it is multiplied, beside it its 8 bits (if it has any), then the other operand (of the widest
+// adapter).  Every role walks it with a cursor of its own (a division per step to find the stage costs as much as the step's products).
 struct RgRing {
-    uint32_t base, stage_bytes;
+    uint32_t base, stage_bytes, low;
     int stages;
-    __device__ RgRing(uint32_t at, int bytes, uint32_t low) : base(at), stage_bytes(kRgTile + low), stages(min(bytes / (int)(kRgTile + low), kRgMaxStages)) {}
+    __device__ RgRing(uint32_t at, int bytes, bool raw, uint32_t low_bytes) : base(at), low(kRgTile + (raw ? kRgRaw : 0))
+    {
+        stage_bytes = low + low_bytes;
+        stages = min(bytes / (int)stage_bytes, kRgMaxStages);
+    }
 };
 struct RgCursor {
     const RgRing& ring;
@@ -184,36 +194,36 @@ struct RgCursor {
 };
 __device__ __forceinline__ uint32_t turn_phase(int turn) { return (uint32_t)(turn / kRgTurns) & 1u; }
 
-// Producer (one thread): hands a stage, what it holds being written, on to the converting warps; stage -1: there is no more.
+// Producer of scale words (one thread): hands a stage on to the converting warps; stage -1: there is no more.
 __device__ __forceinline__ void post_turn(RgCtrl* c, int turn, int stage, uint32_t phase)
 {
     c->turns[turn % kRgTurns] = {stage, (int)phase};
     mbar_arrive(smem_u32(&c->turn[turn % kRgTurns]));   // (releases what was written)
 }
-// Producer of tiles (one thread): the tile at (row, column) into the stage.  `words`: the scale words of the tile's rows.  A bulk copy wants 16-byte boundaries, so theirs begins up to three words early, and takes kRgWords; where that
-// would reach behind the array's end, ordinary loads bring the rest.
-__device__ __forceinline__ void load_tile(RgCtrl* c, const CUtensorMap* map, uint32_t at, int stage, bool raw, int row, int column, int valid, int flags, int r16,
-                                          const uint32_t* words, const uint32_t* words_end)
+// ... the words of half a step's rows into the stage, from `words` on.  A bulk copy wants 16-byte boundaries, so it begins up to three words
+// early, and takes so many more; where that would reach behind the array's end, ordinary loads bring the rest.
+template <bool SECOND>
+__device__ __forceinline__ void load_words(RgCtrl* c, int stage, const uint32_t* words, const uint32_t* words_end)
+{
+    constexpr int kWords = SECOND ? 72 : kRgWords;
+    const uint32_t bar = smem_u32(&c->full[stage]);
+    const uint32_t* from = reinterpret_cast<const uint32_t*>(reinterpret_cast<uintptr_t>(words) & ~(uintptr_t)15);
+    uint32_t bytes = kWords * 4;
+    if (words_end - from < kWords) {
+        bytes = (uint32_t)(words_end - from) * 4u & ~15u;
+        for (const uint32_t* w = from + bytes / 4; w < words_end; ++w) c->words[stage][w - from] = ld_after_wait(w);
+    }
+    mbar_arrive_expect_tx(bar, bytes);
+    if (bytes) bulk_load(smem_u32(c->words[stage]), from, bytes, bar);
+}
+// Producer of tiles (one thread): the half step at (row, column) into the stage.
+template <bool SECOND>
+__device__ __forceinline__ void load_tile(RgCtrl* c, const CUtensorMap* map, uint32_t at, int stage, bool raw, int row, int column)
 {
     const uint32_t bar = smem_u32(&c->full[stage]);
-    if (raw) {
-        const uintptr_t addr = reinterpret_cast<uintptr_t>(words);
-        const uint32_t* from = reinterpret_cast<const uint32_t*>(addr & ~(uintptr_t)15);
-        c->info[stage] = {flags, valid, r16, (int)(addr >> 2) & 3};
-        uint32_t bytes = kRgWords * 4;
-        if (words_end - from < kRgWords) {
-            bytes = (uint32_t)(words_end - from) * 4u & ~15u;
-            for (const uint32_t* w = from + bytes / 4; w < words_end; ++w) c->words[stage][w - from] = ld_after_wait(w);
-        }
-        mbar_arrive_expect_tx(bar, kRgRaw + bytes);
-        tma_load_2d(at, map, bar, column / 2, row);   // (8-bit columns in pairs)
-        if (bytes) bulk_load(smem_u32(c->words[stage]), from, bytes, bar);
-    } else {
-        c->info[stage] = {flags, valid, r16, -1};
-        mbar_arrive_expect_tx(bar, kRgTile);
-        tma_load_2d(at, map, bar, column, row);
-        tma_load_2d(at + kRgHalfTile, map, bar, column + 64, row);
-    }
+    mbar_arrive_expect_tx(bar, raw ? kRgRaw : kRgTile);
+    tma_load_2d(raw ? at + kRgTile : at, map, bar, raw ? column / 2 : column, row);   // (8-bit columns in pairs)
+    if (SECOND && !raw) tma_load_2d(at + kRgHalfTile, map, bar, column + 64, row);
 }
 
 // Issuer of both passes: the steps as they come, told apart by what the producer says about them.  The tile's rows are the product's (first
@@ -235,23 +245,22 @@ __device__ __forceinline__ void issue_steps(RgCtrl* c, const RgRing& ring, uint3
             ++u.turn;
         }
         tc_fence_after();
-        const uint32_t low = u.at + kRgTile;
+        const uint32_t low = u.at + ring.low;
+        const uint64_t bd = umma_desc_k128(low);
         if (SECOND) {
             const uint32_t idesc = umma_idesc_bf16(128, 3 * info.r16) | kIdescMMajorA;
-            const uint64_t ad = umma_desc_m128(u.at), bd = umma_desc_k128(low), bd2 = umma_desc_k128(low + (uint32_t)info.r16 * 384u);
-            if (info.valid > kTileM - 16) {
+            const uint64_t ad = umma_desc_m128(u.at);
+            if (info.valid > 48) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) umma_bf16(acc, ad + (uint64_t)(k * (2048 >> 4)), (k < 4 ? bd : bd2) + (uint64_t)((k & 3) * 2), idesc, k > 0 ? 1u : fresh);
+                for (int k = 0; k < 4; ++k) umma_bf16(acc, ad + (uint64_t)(k * (2048 >> 4)), bd + (uint64_t)(k * 2), idesc, k > 0 ? 1u : fresh);
             } else {
-                for (int k = 0; k * 16 < info.valid; ++k) umma_bf16(acc, ad + (uint64_t)(k * (2048 >> 4)), (k < 4 ? bd : bd2) + (uint64_t)((k & 3) * 2), idesc, k > 0 ? 1u : fresh);
+                for (int k = 0; k * 16 < info.valid; ++k) umma_bf16(acc, ad + (uint64_t)(k * (2048 >> 4)), bd + (uint64_t)(k * 2), idesc, k > 0 ? 1u : fresh);
             }
         } else {
             const uint32_t idesc = umma_idesc_bf16(128, info.r16);
-            const uint64_t ad = umma_desc_k128(u.at), ad2 = umma_desc_k128(u.at + kRgHalfTile);
-            const uint64_t bd = umma_desc_k128(low), bd2 = umma_desc_k128(low + (uint32_t)info.r16 * 128u);
+            const uint64_t ad = umma_desc_k128(u.at);
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                umma_bf16(acc, (k < 4 ? ad : ad2) + (uint64_t)((k & 3) * 2), (k < 4 ? bd : bd2) + (uint64_t)((k & 3) * 2), idesc, k > 0 ? 1u : fresh);
+            for (int k = 0; k < 4; ++k) umma_bf16(acc, ad + (uint64_t)(k * 2), bd + (uint64_t)(k * 2), idesc, k > 0 ? 1u : fresh);
         }
         umma_commit(smem_u32(&c->empty[u.stage]));
         if (flags & kRgLast) {
@@ -262,14 +271,18 @@ __device__ __forceinline__ void issue_steps(RgCtrl* c, const RgRing& ring, uint3
     } while (!(flags & kRgEnd));
 }
 
-// Converting group of both passes: every second tile that is handed on.  Rows behind the last become zeros (in a bf16 tile those that share
-// a step of 16 with it: another token's values times zero would be NaN where they are not finite).
-template <bool E4M3>
+// Converting group of both passes: the half steps that are handed on, in turn.  In the second pass rows behind the last become zeros (in a bf16
+// tile those that share a step of 16 with it: another token's values times zero would be NaN where they are not finite).
+template <bool E4M3, bool SECOND>
 __device__ __forceinline__ void convert_tiles(RgCtrl* c, const RgRing& ring, int group, int wt, int lane, volatile int* abort)
 {
-    const int ch = wt & 3, odd = (wt >> 2) & 1, row0 = wt >> 3, shift = 8 * ((wt & 7) >> 1);
-    const uint32_t to0 = (uint32_t)(odd * kRgHalfTile + row0 * 128 + (((2 * ch + odd) ^ (row0 & 7)) * 16));   // (32 rows on, the swizzle is the same)
-    for (int turn = group;; turn += 2) {
+    // A thread has 16 values of a row (8-bit: four or eight such to a row) in each of kParts rows, kRows apart, where the swizzle is the same: the
+    // 16-byte chunks 2 ch and 2 ch + 1 (of eight) of a row.  In the second pass lanes of the right 64 columns write the odd chunk first, so that
+    // the two sides' lanes, which are 8 KB apart, do not meet on a bank.
+    constexpr int kRows = (SECOND ? 4 : 8) * kRgGroup, kParts = (SECOND ? 64 : 128) / kRows;
+    const int ch = wt & 3, odd = SECOND ? (wt >> 2) & 1 : 0, row0 = SECOND ? wt >> 3 : wt >> 2;
+    const uint32_t to0 = (uint32_t)(odd * kRgHalfTile + row0 * 128 + (((2 * ch + odd) ^ (row0 & 7)) * 16));
+    for (int turn = group;; turn += kRgGroups) {
         const int k = turn % kRgTurns;
         bool ok = mbar_wait_warp(smem_u32(&c->turn[k]), turn_phase(turn), abort);
         __syncwarp();
@@ -280,38 +293,38 @@ __device__ __forceinline__ void convert_tiles(RgCtrl* c, const RgRing& ring, int
         __syncwarp();
         const uint32_t at = ring.base + (uint32_t)stage * ring.stage_bytes;
         const RgInfo info = c->info[stage];
-        // 16 values of a row: the 16-byte chunks 2 ch and 2 ch + 1 (of eight) of a half's row, swizzled by the row.  Lanes of the second half
-        // take the odd chunk first, so that the two halves' lanes, which are 16 KB apart, do not meet on a bank.
-        uint2 v[4][2];
-        uint32_t byte[4];
+        const int shift = 8 * (SECOND ? (wt & 7) >> 1 : (ch >> 1) + (info.flags & kRgRight ? 2 : 0));
+        uint2 v[kParts][2];
+        uint32_t byte[kParts], most = 0;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const uint32_t from = at + (uint32_t)(q * (kRgRaw / 4) + wt * 16);
-            v[q][0] = ld_smem_v2(from + odd * 8);
-            v[q][1] = ld_smem_v2(from + 8 - odd * 8);
-            byte[q] = (c->words[stage][(info.word & 3) + row0 + 32 * q] >> shift) & 0xffu;
+        for (int q = 0; q < kParts; ++q) {
+            const uint4 w = ld_smem_v4(at + (uint32_t)(kRgTile + q * (kRgRaw / kParts) + wt * 16));
+            v[q][0] = odd ? make_uint2(w.z, w.w) : make_uint2(w.x, w.y);
+            v[q][1] = odd ? make_uint2(w.x, w.y) : make_uint2(w.z, w.w);
+            byte[q] = (c->words[stage][(info.word & 3) + row0 + kRows * q] >> shift) & 0xffu;
+            most = max(most, byte[q]);
         }
-        const bool usual = info.valid == kTileM && max(max(byte[0], byte[1]), max(byte[2], byte[3])) <= Decoder<E4M3>::kMost;
-        if (group_any(group, !ok)) return;   // (everybody has the tile's values, so their place may be written; or a wait gave up)
+        const bool usual = (!SECOND || info.valid == 64) && most <= Decoder<E4M3>::kMost;
+        if (!ok) return;   // (a wait gave up)
         const uint32_t to = at + to0;
         if (info.word >= 0 && usual) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
+            for (int q = 0; q < kParts; ++q) {
                 const Decoder<E4M3> decode(byte[q]);
-                st_smem_v4(to + (uint32_t)(q * 32 * 128), decode.eight(v[q][0]));
-                st_smem_v4((to ^ 16u) + (uint32_t)(q * 32 * 128), decode.eight(v[q][1]));
+                st_smem_v4(to + (uint32_t)(q * kRows * 128), decode.eight(v[q][0]));
+                st_smem_v4((to ^ 16u) + (uint32_t)(q * kRows * 128), decode.eight(v[q][1]));
             }
         } else if (info.word >= 0) {
 #pragma unroll 1
-            for (int q = 0; q < 4; ++q) {
-                const bool there = row0 + 32 * q < info.valid;
+            for (int q = 0; q < kParts; ++q) {
+                const bool there = !SECOND || row0 + kRows * q < info.valid;
                 const uint4 zero = make_uint4(0, 0, 0, 0);
-                st_smem_v4(to + (uint32_t)(q * 32 * 128), there ? decode8<E4M3>(v[0][0], byte[0]) : zero);
-                st_smem_v4((to ^ 16u) + (uint32_t)(q * 32 * 128), there ? decode8<E4M3>(v[0][1], byte[0]) : zero);
+                st_smem_v4(to + (uint32_t)(q * kRows * 128), there ? decode8<E4M3>(v[0][0], byte[0]) : zero);
+                st_smem_v4((to ^ 16u) + (uint32_t)(q * kRows * 128), there ? decode8<E4M3>(v[0][1], byte[0]) : zero);
 #pragma unroll
-                for (int i = 0; i < 3; ++i) { v[i][0] = v[i + 1][0]; v[i][1] = v[i + 1][1]; byte[i] = byte[i + 1]; }
+                for (int i = 0; i + 1 < kParts; ++i) { v[i][0] = v[i + 1][0]; v[i][1] = v[i + 1][1]; byte[i] = byte[i + 1]; }
             }
-        } else {
+        } else if (SECOND) {
             const int rows = 16 - (info.valid & 15);
             for (int e = wt; e < rows * 16; e += 32 * kRgGroup) {
                 const int row = info.valid + (e >> 4);
@@ -338,22 +351,22 @@ __device__ __forceinline__ RgShare share_of(const RgLine& line, int item, int n,
     const int first = line.part_of(item);
     return {first, line.part_of(item + n - 1), k == first ? 1 : 0};   // (the others begin behind the item's first step)
 }
-// After all finishing warps have written this CTA's partial result: whether it is the last one of the item's.
-__device__ __forceinline__ bool arrive_last(RgCtrl* c, const RowsGradParams& p, const RgShare& s)
+// After all finishing warps have written this CTA's partial result: if it is the last one of the item's, the CTA joins them later.
+__device__ __forceinline__ void arrive(RgCtrl* c, const RowsGradParams& p, const RgShare& s, int job, int slot, int at, int valid)
 {
     __threadfence();
     finish_barrier();
     if (threadIdx.x == 64) {   // (the first of them)
         const int n = atomicAdd(p.arrived + s.first, 1);
-        c->last = n == s.last - s.first;
-        if (c->last) atomicExch(p.arrived + s.first, 0);   // (for the next call)
+        if (n == s.last - s.first) {
+            atomicExch(p.arrived + s.first, 0);   // (for the next call)
+            c->joins[c->n_joins++] = {job, slot, s.first, s.last, at, valid};
+        }
         __threadfence();
     }
-    finish_barrier();
-    return c->last != 0;
 }
-// Four values of the joined result: up to eight parts' loads in flight
-__device__ __forceinline__ float4 join(const RowsGradParams& p, const RgShare& s, int at)
+// Four values of the joined result, the parts added in their order, eight of them in flight.
+__device__ __forceinline__ float4 joined(const RowsGradParams& p, const RgJoin& s, int at)
 {
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int k0 = s.first; k0 <= s.last; k0 += 8) {
@@ -393,6 +406,9 @@ __device__ __forceinline__ void flag_segment(const RowsGradParams& p, const RgSe
     if (slot_rank(p.snap[1], seg.sT) != r) atomicOr(p.status[1], LML_FLAG_BAD_SLOT);
 }
 
+// Halves of a step with something in them: of its 128 columns (first pass) or rows (second) `from` and more are left of `all`.
+__device__ __forceinline__ int halves(int from, int all) { return all - from > 64 ? 2 : 1; }
+
 // ---- first pass ------------------------------------------------------------------------------------------
 // This CTA's part of the line, item by item: pieces in order, of each x, then dy.
 struct ShrinkTasks {
@@ -422,13 +438,14 @@ struct ShrinkTasks {
     __device__ int item() const { return w - step; }
 };
 
-// Three bf16 values whose sum is x; an x that is not finite stands in the first alone.
-__device__ __forceinline__ void split3(float x, float (&part)[3])
+// Three bf16 values whose sum is x, for two x; an x that is not finite stands in the first alone.
+__device__ __forceinline__ void split3(float x, float y, uint32_t (&part)[3])
 {
-    part[0] = __bfloat162float(__float2bfloat16_rn(x));
-    const float rest = fabsf(part[0]) < INFINITY ? x - part[0] : 0.f;
-    part[1] = __bfloat162float(__float2bfloat16_rn(rest));
-    part[2] = rest - part[1];
+    part[0] = pack_bf16(x, y);
+    x = fabsf(bf16_lo(part[0])) < INFINITY ? x - bf16_lo(part[0]) : 0.f;
+    y = fabsf(bf16_hi(part[0])) < INFINITY ? y - bf16_hi(part[0]) : 0.f;
+    part[1] = pack_bf16(x, y);
+    part[2] = pack_bf16(x - bf16_lo(part[1]), y - bf16_hi(part[1]));
 }
 
 template <int FMT>
@@ -475,45 +492,58 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_shrink_kernel(const __grid
     const RgLine line(c->pre[kRgSegs] * (p.tiles[0] + p.tiles[1]));
     const int w0 = line.begin((int)blockIdx.x), w1 = line.begin((int)blockIdx.x + 1);
 
-    const RgRing ring(smem, p.ring, (uint32_t)p.r16 * 256u);
+    const RgRing ring(smem, p.ring, FMT != kBf16, (uint32_t)p.r16 * 128u);
+    // Every half step of this CTA, for a producer: wait for its stage, then `f`.
+    auto each = [&](auto&& f) {
+        RgCursor u(ring);
+        for (ShrinkTasks t(p, c, w0, w1); t.next();) {
+            const bool end = t.w + t.n == w1;
+            int k = t.step * 128;
+            for (int left = t.n; left > 0; --left, k += 128) {
+                const int n = halves(k, p.d[t.job]);
+                for (int half = 0; half < n; ++half, u.advance()) {
+                    if (!mbar_wait(smem_u32(&c->empty[u.stage]), u.phase ^ 1u, abort)) return u.turn;
+                    f(u, t, k, half, left == 1 && half + 1 == n, end);
+                }
+            }
+        }
+        return u.turn;
+    };
     if (w0 < w1) {
         if (warp == 0) {
-            if (elect_one()) {
-                RgCursor u(ring);
-                const uint32_t* words_end = p.scales + (size_t)kept_groups(p.d[0]) * p.T;
-                for (ShrinkTasks t(p, c, w0, w1); t.next();) {
-                    const bool raw = FMT != kBf16 && t.job == 0;
-                    const uint32_t* words = p.scales + (size_t)t.step * p.T + t.row;
-                    const CUtensorMap* map = &p.map[t.job];
-                    const int r16 = chunks_of_rank(p.snap[t.job].rank[t.slot]) * kChunk, end = t.w + t.n == w1 ? kRgLast | kRgEnd : kRgLast;
-                    int flags = kRgFirst | (raw ? kRgTouched : 0), k = t.step * 128;
-                    for (int left = t.n; left > 0; --left, k += 128, words += p.T, u.advance()) {
-                        if (!mbar_wait(smem_u32(&c->empty[u.stage]), u.phase ^ 1u, abort)) break;
-                        if (left == 1) flags |= end;
-                        load_tile(c, map, u.at, u.stage, raw, t.row, k, t.valid, flags, r16, words, words_end);
-                        if (raw) { post_turn(c, u.turn, u.stage, u.phase); ++u.turn; }
-                        flags &= ~kRgFirst;
-                    }
-                }
-                if (FMT != kBf16)
-                    for (int k = 0; k < 2; ++k) post_turn(c, u.turn + k, -1, 0);
-            }
+            if (elect_one())
+                each([&](RgCursor& u, const ShrinkTasks& t, int k, int half, bool, bool) {
+                    load_tile<false>(c, &p.map[0][t.job], u.at, u.stage, FMT != kBf16 && t.job == 0, t.row, k + 64 * half);
+                });
         } else if (warp == kRgOther) {
+            if (elect_one())
+                each([&](RgCursor& u, const ShrinkTasks& t, int k, int half, bool last, bool end) {
+                    const int chunks = chunks_of_rank(p.snap[t.job].rank[t.slot]);
+                    const bool raw = FMT != kBf16 && t.job == 0;
+                    int flags = raw ? kRgTouched : 0;
+                    if (half) flags |= kRgRight;
+                    else if (k == t.step * 128) flags |= kRgFirst;
+                    if (last) flags |= end ? kRgLast | kRgEnd : kRgLast;
+                    c->info[u.stage] = {flags, t.valid, chunks * kChunk,
+                                        raw ? (int)(reinterpret_cast<uintptr_t>(p.scales + (size_t)(k >> 7) * p.T + t.row) >> 2) & 3 : -1};
+                    const uint32_t bar = smem_u32(&c->full[u.stage]);
+                    mbar_arrive_expect_tx(bar, (uint32_t)chunks * (kChunk * 128u));
+                    tma_load_2d(u.at + ring.low, &p.low[t.job][chunks - 1], bar, k + 64 * half, t.slot * kRankPad);
+                });
+        } else if (warp == kRgWordsWarp) {
             if (elect_one()) {
-                RgCursor u(ring);
-                for (ShrinkTasks t(p, c, w0, w1); t.next();) {
-                    const int chunks = chunks_of_rank(p.snap[t.job].rank[t.slot]), row = t.slot * kRankPad;
-                    const uint32_t half = (uint32_t)chunks * kChunk * 128u;
-                    const CUtensorMap* low = &p.low[t.job][chunks - 1];
-                    int k = t.step * 128;
-                    for (int left = t.n; left > 0; --left, k += 128, u.advance()) {
-                        if (!mbar_wait(smem_u32(&c->empty[u.stage]), u.phase ^ 1u, abort)) break;
-                        const uint32_t bar = smem_u32(&c->full[u.stage]);
-                        mbar_arrive_expect_tx(bar, 2 * half);
-                        tma_load_2d(u.at + kRgTile, low, bar, k, row);
-                        tma_load_2d(u.at + kRgTile + half, low, bar, k + 64, row);
+                const uint32_t* words_end = p.scales + (size_t)kept_groups(p.d[0]) * p.T;
+                const int turns = each([&](RgCursor& u, const ShrinkTasks& t, int k, int, bool, bool) {
+                    if (FMT == kBf16 || t.job) {
+                        mbar_arrive(smem_u32(&c->full[u.stage]));
+                    } else {
+                        load_words<false>(c, u.stage, p.scales + (size_t)(k >> 7) * p.T + t.row, words_end);
+                        post_turn(c, u.turn, u.stage, u.phase);
+                        ++u.turn;
                     }
-                }
+                });
+                if (FMT != kBf16)
+                    for (int k = 0; k < kRgGroups; ++k) post_turn(c, turns + k, -1, 0);
             }
         } else if (warp == 1) {
             if (elect_one()) issue_steps<false>(c, ring, tmem, (uint32_t)p.r16, abort);
@@ -534,56 +564,64 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_shrink_kernel(const __grid
                 uint8_t* out = p.pieces[t.job] + (size_t)t.piece * kRgPiece;
                 float* mine_at = p.partial + (size_t)(2 * blockIdx.x + share.slot) * kRgPartial;
                 // (r16 is a multiple of 16: the swizzle goes by j alone)
-                uint8_t* half = out + (size_t)(row >> 6) * (r16 * 384) + (row & 7) * 2;
                 const bool there = row < t.valid;   // (rows behind the segment, columns behind the rank: whatever they hold)
                 const uint32_t from = tmem + (items & 1) * (uint32_t)p.r16 + ((uint32_t)((warp & 3) * 32) << 16);
+                // Two lanes share out two columns, so that each has both tokens of one: 4 bytes per store
+                const int odd = lane & 1;
+                uint8_t* const pair_at = out + (size_t)(row >> 6) * (r16 * 384) + (row & 6) * 2;
 #pragma unroll 1
-                for (int j = 0; j < r16; j += 4) {
-                    uint32_t v[4];
-                    tmem_ld_32x4(from + (uint32_t)j, v);
+                for (int j = 0; j < r16; j += 8) {
+                    uint32_t v[8];
+                    tmem_ld_32x8(from + (uint32_t)j, v);
                     tmem_ld_wait();
+                    if (!whole) {
+                        float* to = mine_at + j * 128 + row;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (whole) {
-                            float part[3];
-                            split3(there && j + e < r ? __uint_as_float(v[e]) * sc : 0.f, part);
-                            uint8_t* at = half + (j + e) * 128 + ((((row & 63) >> 3) ^ ((j + e) & 7)) * 16);
+                        for (int e = 0; e < 8; ++e) to[e * 128] = __uint_as_float(v[e]);
+                        continue;
+                    }
 #pragma unroll
-                            for (int k = 0; k < 3; ++k) *reinterpret_cast<__nv_bfloat16*>(at + k * r16 * 128) = __float2bfloat16_rn(part[k]);
-                        } else {
-                            mine_at[(j + e) * 128 + row] = __uint_as_float(v[e]);
-                        }
+                    for (int e = 0; e < 8; e += 2) {
+                        const float x = there && j + e < r ? __uint_as_float(v[e]) * sc : 0.f, y = there && j + e + 1 < r ? __uint_as_float(v[e + 1]) * sc : 0.f;
+                        const float got = __shfl_xor_sync(0xffffffffu, odd ? x : y, 1);
+                        uint32_t part[3];
+                        split3(odd ? got : x, odd ? y : got, part);
+                        uint8_t* at = pair_at + (j + e + odd) * 128 + ((((row & 63) >> 3) ^ (e + odd)) * 16);
+#pragma unroll
+                        for (int k = 0; k < 3; ++k) *reinterpret_cast<uint32_t*>(at + k * r16 * 128) = part[k];
                     }
                 }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&c->acc_free[items & 1]));
-                if (!whole && arrive_last(c, p, share)) {
-                    for (int e = wt; e < r16 * 32; e += 32 * kRgFinish) {   // four tokens of one column
-                        const int j = e >> 5, t4 = (e & 31) * 4;
-                        const float4 v = join(p, share, e * 4);
-                        const float x[4] = {v.x, v.y, v.z, v.w};
-                        float part[4][3];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) split3(j < r && t4 + i < t.valid ? x[i] * sc : 0.f, part[i]);
-#pragma unroll
-                        for (int k = 0; k < 3; ++k) {
-                            const int line_at = k * r16 + j;
-                            *reinterpret_cast<uint2*>(out + (size_t)(t4 >> 6) * (r16 * 384) + line_at * 128 + ((((t4 & 63) >> 3) ^ (line_at & 7)) * 16) + (t4 & 4) * 2) =
-                                make_uint2(pack_bf16(part[0][k], part[1][k]), pack_bf16(part[2][k], part[3][k]));
-                        }
-                    }
-                }
+                if (!whole) arrive(c, p, share, t.job, t.slot, t.piece, t.valid);
             }
             fence_proxy_async_all();          // the pieces are read by bulk copies
         } else if (FMT != kBf16) {
             const int group = (warp - kRgFirstConv) / kRgGroup;
-            convert_tiles<FMT == kE4m3>(c, ring, group, tid - 32 * (kRgFirstConv + group * kRgGroup), lane, abort);
+            convert_tiles<FMT == kE4m3, false>(c, ring, group, tid - 32 * (kRgFirstConv + group * kRgGroup), lane, abort);
         }
     }
     __syncwarp();
     if (*abort) __nanosleep(50000);   // gave up: let copies still in flight land before the CTA goes away
     __syncthreads();
+    for (int i = 0; i < c->n_joins; ++i) {
+        const RgJoin s = c->joins[i];
+        const int r = p.snap[s.job].rank[s.slot], r16 = chunks_of_rank(r) * kChunk;
+        const float sc = p.snap[s.job].scale[s.slot];
+        for (int e = tid; e < r16 * 32; e += kRgThreads) {   // four tokens of one column
+            const int j = e >> 5, t4 = (e & 31) * 4;
+            const float4 v = joined(p, s, e * 4);
+            const auto value = [&](float x, int k) { return j < r && t4 + k < s.valid ? x * sc : 0.f; };
+            uint32_t part[2][3];
+            split3(value(v.x, 0), value(v.y, 1), part[0]);
+            split3(value(v.z, 2), value(v.w, 3), part[1]);
+            uint8_t* at = p.pieces[s.job] + (size_t)s.at * kRgPiece + (size_t)(t4 >> 6) * (r16 * 384) + j * 128 + ((((t4 & 63) >> 3) ^ (j & 7)) * 16) + (t4 & 4) * 2;
+#pragma unroll
+            for (int k = 0; k < 3; ++k) *reinterpret_cast<uint2*>(at + k * r16 * 128) = make_uint2(part[0][k], part[1][k]);
+        }
+        fence_proxy_async_all();
+    }
     if (tid == 0 && *abort) atomicOr(p.status[0], LML_FLAG_TIMEOUT);
     if (warp == 1) {
         tc_fence_after();
@@ -600,7 +638,7 @@ struct GradTasks {
     unsigned long long mask;   // slots from here on
     int w, end, base = 0;   // base: of the slot at hand
     int slot = 0, units = 0, tile = 0, a = 0, b = 0;
-    __device__ GradTasks(const RowsGradParams& p_, const RgCtrl* c_, int w0, int w1) : p(p_), c(c_), mask(c_->used), w(w0), end(w1) {}
+    __device__ GradTasks(const RowsGradParams& p_, const RgCtrl* c_, int w0, int w1) : p(p_), c(c_), mask(c_->used()), w(w0), end(w1) {}
     __device__ void next_slot()
     {
         base += units * p.all_tiles;
@@ -695,7 +733,7 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_grad_kernel(const __grid_c
         c->len[tid] = mine_units;   // (for now)
     }
     if (mine) {
-        atomicOr(&c->used, 1ull << seg.s);
+        atomicOr(&c->used_half[seg.s >> 5], 1u << (seg.s & 31));
         atomicAdd(&c->units[seg.s], mine_units);
     }
     __syncthreads();
@@ -712,49 +750,60 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_grad_kernel(const __grid_c
     }
     __syncthreads();
     int total = 0;
-    for (unsigned long long m = c->used; m; m &= m - 1ull) total += p.whole_items ? 1 : c->units[__ffsll((long long)m) - 1];
+    for (unsigned long long m = c->used(); m; m &= m - 1ull) total += p.whole_items ? 1 : c->units[__ffsll((long long)m) - 1];
     const RgLine line(total * p.all_tiles);
     const int w0 = p.whole_items ? (int)blockIdx.x : line.begin((int)blockIdx.x), w1 = p.whole_items ? line.W : line.begin((int)blockIdx.x + 1);
 
-    const RgRing ring(smem, p.ring, (uint32_t)p.r16 * 768u);
+    const RgRing ring(smem, p.ring, FMT != kBf16, (uint32_t)p.r16 * 384u);
+    auto each = [&](auto&& f) {   // (see rows_shrink_kernel)
+        RgCursor u(ring);
+        for (GradTasks t(p, c, w0, w1); t.next();) {
+            const bool raw = FMT != kBf16 && t.job() == 0, end = t.last();
+            bool first = true;
+            for (RgPieces v(c, t); v.next();) {
+                const int valid = v.valid(), n = halves(0, valid);
+                for (int half = 0; half < n; ++half, u.advance()) {
+                    if (!mbar_wait(smem_u32(&c->empty[u.stage]), u.phase ^ 1u, abort)) return u.turn;
+                    const int rows = min(valid - 64 * half, 64);
+                    int flags = raw || (rows & 15) ? kRgTouched : 0;
+                    if (first) flags |= kRgFirst;
+                    first = false;
+                    if (v.left == 0 && half + 1 == n) flags |= end ? kRgLast | kRgEnd : kRgLast;
+                    f(u, t, v, raw, half, rows, flags);
+                }
+            }
+        }
+        return u.turn;
+    };
     if (w0 < w1) {
         if (warp == 0) {
-            if (elect_one()) {
-                RgCursor u(ring);
-                const uint32_t* words_end = p.scales + (size_t)kept_groups(p.d[0]) * p.T;
-                for (GradTasks t(p, c, w0, w1); t.next();) {
-                    const int job = t.job(), c0 = t.column(), r16 = chunks_of_rank(p.snap[0].rank[t.slot]) * kChunk, end = t.last() ? kRgLast | kRgEnd : kRgLast;
-                    const bool raw = FMT != kBf16 && job == 0;
-                    const uint32_t* words = p.scales + (size_t)(c0 >> 7) * p.T;
-                    const CUtensorMap* map = &p.map[job];
-                    int flags = kRgFirst;
-                    for (RgPieces v(c, t); v.next(); u.advance()) {
-                        const int row = v.row(), valid = v.valid();
-                        if (v.left == 0) flags |= end;
-                        if (!mbar_wait(smem_u32(&c->empty[u.stage]), u.phase ^ 1u, abort)) break;
-                        const bool touched = raw || (valid & 15);
-                        load_tile(c, map, u.at, u.stage, raw, row, c0, valid, touched ? flags | kRgTouched : flags, r16, words + row, words_end);
-                        if (touched) { post_turn(c, u.turn, u.stage, u.phase); ++u.turn; }
-                        flags = 0;
-                    }
-                }
-                for (int k = 0; k < 2; ++k) post_turn(c, u.turn + k, -1, 0);
-            }
+            if (elect_one())
+                each([&](RgCursor& u, const GradTasks& t, const RgPieces& v, bool raw, int half, int, int) {
+                    load_tile<true>(c, &p.map[1][t.job()], u.at, u.stage, raw, v.row() + 64 * half, t.column());
+                });
         } else if (warp == kRgOther) {
             if (elect_one()) {
                 grid_dependency_wait();   // (the tiles are on their way meanwhile)
                 fence_proxy_async_all();
-                RgCursor u(ring);
-                for (GradTasks t(p, c, w0, w1); t.next();) {
-                    const uint32_t low = (uint32_t)(chunks_of_rank(p.snap[0].rank[t.slot]) * kChunk) * 768u;
-                    const uint8_t* pieces = p.pieces[t.job() ^ 1];   // (u for dy, v for x)
-                    for (RgPieces v(c, t); v.next(); u.advance()) {
-                        if (!mbar_wait(smem_u32(&c->empty[u.stage]), u.phase ^ 1u, abort)) break;
-                        const uint32_t bar = smem_u32(&c->full[u.stage]);
-                        mbar_arrive_expect_tx(bar, low);
-                        bulk_load(u.at + kRgTile, pieces + v.at(), low, bar);
-                    }
-                }
+                each([&](RgCursor& u, const GradTasks& t, const RgPieces& v, bool raw, int half, int rows, int flags) {
+                    const int r16 = chunks_of_rank(p.snap[0].rank[t.slot]) * kChunk;
+                    const uint32_t low = (uint32_t)r16 * 384u;
+                    c->info[u.stage] = {flags, rows, r16,
+                                        raw ? (int)(reinterpret_cast<uintptr_t>(p.scales + (size_t)t.tile * p.T + v.row()) >> 2) & 3 : -1};
+                    const uint32_t bar = smem_u32(&c->full[u.stage]);
+                    mbar_arrive_expect_tx(bar, low);
+                    bulk_load(u.at + ring.low, p.pieces[t.job() ^ 1] + v.at() + half * low, low, bar);   // (u for dy, v for x)
+                });
+            }
+        } else if (warp == kRgWordsWarp) {
+            if (elect_one()) {
+                const uint32_t* words_end = p.scales + (size_t)kept_groups(p.d[0]) * p.T;
+                const int turns = each([&](RgCursor& u, const GradTasks& t, const RgPieces& v, bool raw, int half, int, int flags) {
+                    if (raw) load_words<true>(c, u.stage, p.scales + (size_t)t.tile * p.T + v.row() + 64 * half, words_end);
+                    else mbar_arrive(smem_u32(&c->full[u.stage]));
+                    if (flags & kRgTouched) { post_turn(c, u.turn, u.stage, u.phase); ++u.turn; }
+                });
+                for (int k = 0; k < kRgGroups; ++k) post_turn(c, turns + k, -1, 0);
             }
         } else if (warp == 1) {
             if (elect_one()) issue_steps<true>(c, ring, tmem, 3u * (uint32_t)p.r16, abort);
@@ -765,80 +814,118 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_grad_kernel(const __grid_c
                 mbar_wait_warp(smem_u32(&c->acc_full[items & 1]), (items >> 1) & 1, abort);
                 __syncwarp();
                 tc_fence_after();
-                // The sums: lane = column.  Partial results: dA [j][column], dB [column][j].
+                // The sums, 16 columns of the accumulator at a time: lane = column of x or dy.  Partial results: dA [j][column], dB [column][j].
+                // dA is written as it stands, 128 bytes of a row per store; dB by way of shared memory, 64 bytes of a column's row.  (Four at a
+                // time straight to their places, each asked about: 205 us for the call where this took 176.)
                 const int job = t.job(), c0 = t.column();
-                const int r = p.snap[0].rank[t.slot], r16 = chunks_of_rank(r) * kChunk, row = (warp & 3) * 32 + lane, d = p.d[job];
-                const bool whole = t.whole();
-                float* dst;   // where (column, j) goes: to a partial result every one of them, to the gradients those that there are
-                int stride = 1;   // between two j
-                if (!whole) {
-                    dst = p.partial + (size_t)(2 * blockIdx.x + (line.part_of(t.item()) == (int)blockIdx.x ? 1 : 0)) * kRgPartial + (job == 0 ? row : row * r16);
-                    if (job == 0) stride = 128;
-                } else if (job == 0) {
-                    dst = p.out[0] + (size_t)t.slot * kRankPad * d + c0 + row;
-                    stride = d;
-                } else {
-                    dst = p.out[1] + ((size_t)t.slot * d + c0 + row) * kRankPad;
-                }
-                const uint32_t from = tmem + (items & 1) * 3u * (uint32_t)p.r16 + ((uint32_t)((warp & 3) * 32) << 16);
-                const bool there = !whole || c0 + row < d, add = whole && p.accumulate;
-                const int most = whole ? r : r16;
+                const int r = p.snap[0].rank[t.slot], r16 = chunks_of_rank(r) * kChunk, col0 = (warp & 3) * 32, d = p.d[job];
+                const bool whole = t.whole(), add = whole && p.accumulate;
+                float* dst = p.partial + (size_t)(2 * blockIdx.x + (!whole && line.part_of(t.item()) == (int)blockIdx.x ? 1 : 0)) * kRgPartial;
+                if (whole) dst = p.out[job] + (size_t)t.slot * kRankPad * d + (job == 0 ? c0 : c0 * kRankPad);
+                const int stride = !whole ? (job == 0 ? 128 : r16) : job == 0 ? d : kRankPad;   // between two j, or two columns
+                const int most = whole ? r : r16, columns = whole ? d - c0 : 128;               // of them that there are
+                const uint32_t from = tmem + (items & 1) * 3u * (uint32_t)p.r16 + ((uint32_t)col0 << 16);
 #pragma unroll 1
-                for (int j = 0; j < r16; j += 4) {
-                    uint32_t h[4], m[4], l[4];
-                    tmem_ld_32x4(from + (uint32_t)j, h);
-                    tmem_ld_32x4(from + (uint32_t)(r16 + j), m);
-                    tmem_ld_32x4(from + (uint32_t)(2 * r16 + j), l);
-                    tmem_ld_wait();
-                    float s[4];
+                for (int j = 0; j < r16; j += 16) {
+                    float s[16];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[e] = __uint_as_float(h[e]) + (__uint_as_float(m[e]) + __uint_as_float(l[e]));
-                    if (there && job == 1 && j + 4 <= most && !add) {
-                        *reinterpret_cast<float4*>(dst) = make_float4(s[0], s[1], s[2], s[3]);
-                        dst += 4;
-                    } else {
+                    for (int k = 0; k < 16; k += 8) {
+                        uint32_t h[8], m[8], l[8];
+                        tmem_ld_32x8(from + (uint32_t)(j + k), h);
+                        tmem_ld_32x8(from + (uint32_t)(r16 + j + k), m);
+                        tmem_ld_32x8(from + (uint32_t)(2 * r16 + j + k), l);
+                        tmem_ld_wait();
 #pragma unroll
-                        for (int e = 0; e < 4; ++e, dst += stride)
-                            if (there && j + e < most) *dst = add ? *dst + s[e] : s[e];
+                        for (int e = 0; e < 8; ++e) s[k + e] = __uint_as_float(h[e]) + (__uint_as_float(m[e]) + __uint_as_float(l[e]));
+                    }
+                    if (job == 0) {
+                        float* to = dst + (size_t)j * stride + col0 + lane;
+                        if (!add && j + 16 <= most && col0 + 32 <= columns) {
+#pragma unroll
+                            for (int e = 0; e < 16; ++e, to += stride) *to = s[e];
+                        } else if (col0 + lane < columns) {
+                            if (add) {
+#pragma unroll
+                                for (int e = 0; e < 16; ++e)
+                                    if (j + e < most) s[e] += to[(size_t)e * stride];
+                            }
+#pragma unroll
+                            for (int e = 0; e < 16; ++e)
+                                if (j + e < most) to[(size_t)e * stride] = s[e];
+                        }
+                        continue;
+                    }
+                    float4(*turned)[5] = c->turned[warp & 3];   // [column][j / 4], and a place that spreads the columns over the banks
+                    __syncwarp();
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) turned[lane][e] = make_float4(s[4 * e], s[4 * e + 1], s[4 * e + 2], s[4 * e + 3]);
+                    __syncwarp();
+                    const int j4 = j + (lane & 3) * 4;
+                    float* const to0 = dst + (size_t)(col0 + (lane >> 2)) * stride + j4;
+                    if (!add && j + 16 <= most && col0 + 32 <= columns) {
+                        float* to = to0;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e, to += 8 * stride) *reinterpret_cast<float4*>(to) = turned[e * 8 + (lane >> 2)][lane & 3];
+                        continue;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int column = e * 8 + (lane >> 2);
+                        float4 x = turned[column][lane & 3];
+                        float* to = to0 + (size_t)(e * 8) * stride;
+                        if (col0 + column >= columns) continue;
+                        if (j4 + 4 <= most) {
+                            if (add) {
+                                const float4 o = *reinterpret_cast<const float4*>(to);
+                                x = make_float4(o.x + x.x, o.y + x.y, o.z + x.z, o.w + x.w);
+                            }
+                            *reinterpret_cast<float4*>(to) = x;
+                        } else {
+                            const float f[3] = {x.x, x.y, x.z};   // (less than four)
+#pragma unroll
+                            for (int i = 0; i < 3; ++i)
+                                if (j4 + i < most) to[i] = add ? to[i] + f[i] : f[i];
+                        }
                     }
                 }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&c->acc_free[items & 1]));
                 if (whole) continue;
-                const RgShare share = share_of(line, t.item(), t.units, (int)blockIdx.x);
-                if (arrive_last(c, p, share)) {
-                    const int per = job == 0 ? 32 : r16 / 4;   // float4 per row of the partial results
-                    float* out = p.out[job] + (size_t)t.slot * kRankPad * d;
-                    for (int e = wt; e < r16 * 32; e += 32 * kRgFinish) {
-                        const int line_at = e / per, col = (e % per) * 4;
-                        const int j = job == 0 ? line_at : col, n = c0 + (job == 0 ? col : line_at);
-                        if (j >= r || n >= d) continue;
-                        const float4 s = join(p, share, e * 4);
-                        float* dst = job == 0 ? out + (size_t)j * d + n : out + (size_t)n * kRankPad + j;
-                        if (job == 0 || j + 4 <= r) {   // (d is a multiple of 8)
-                            const float4 o = p.accumulate ? *reinterpret_cast<const float4*>(dst) : make_float4(0.f, 0.f, 0.f, 0.f);
-                            *reinterpret_cast<float4*>(dst) = make_float4(o.x + s.x, o.y + s.y, o.z + s.z, o.w + s.w);
-                        } else {
-                            const float w[3] = {s.x, s.y, s.z};   // (less than four columns)
-#pragma unroll
-                            for (int i = 0; i < 3; ++i)
-                                if (j + i < r) dst[i] = p.accumulate ? dst[i] + w[i] : w[i];
-                        }
-                    }
-                }
+                arrive(c, p, share_of(line, t.item(), t.units, (int)blockIdx.x), job, t.slot, c0, 0);
             }
         } else {
             const int group = (warp - kRgFirstConv) / kRgGroup;
-            convert_tiles<FMT == kE4m3>(c, ring, group, tid - 32 * (kRgFirstConv + group * kRgGroup), lane, abort);
+            convert_tiles<FMT == kE4m3, true>(c, ring, group, tid - 32 * (kRgFirstConv + group * kRgGroup), lane, abort);
         }
     }
     __syncwarp();
     if (*abort) __nanosleep(50000);
     grid_dependency_wait();   // (a CTA without units too: who waits for this grid has waited for the pieces' writers)
     __syncthreads();
+    for (int i = 0; i < c->n_joins; ++i) {
+        const RgJoin s = c->joins[i];
+        const int r = p.snap[0].rank[s.slot], r16 = chunks_of_rank(r) * kChunk, d = p.d[s.job], per = s.job == 0 ? 32 : r16 / 4;   // float4 per row of the partial results
+        float* out = p.out[s.job] + (size_t)s.slot * kRankPad * d;
+        for (int e = tid; e < r16 * 32; e += kRgThreads) {
+            const int line_at = e / per, col = (e % per) * 4;
+            const int j = s.job == 0 ? line_at : col, n = s.at + (s.job == 0 ? col : line_at);
+            if (j >= r || n >= d) continue;
+            const float4 v = joined(p, s, e * 4);
+            float* dst = s.job == 0 ? out + (size_t)j * d + n : out + (size_t)n * kRankPad + j;
+            if (s.job == 0 || j + 4 <= r) {   // (d is a multiple of 8)
+                const float4 o = p.accumulate ? *reinterpret_cast<const float4*>(dst) : make_float4(0.f, 0.f, 0.f, 0.f);
+                *reinterpret_cast<float4*>(dst) = make_float4(o.x + v.x, o.y + v.y, o.z + v.z, o.w + v.w);
+            } else {
+                const float w[3] = {v.x, v.y, v.z};   // (less than four columns)
+#pragma unroll
+                for (int k = 0; k < 3; ++k)
+                    if (j + k < r) dst[k] = p.accumulate ? dst[k] + w[k] : w[k];
+            }
+        }
+    }
     if (!p.accumulate) {      // adapters without a token
-        for (unsigned long long m = p.live & ~c->used; m; m &= m - 1ull) {
+        for (unsigned long long m = p.live & ~c->used(); m; m &= m - 1ull) {
             const int slot = __ffsll((long long)m) - 1, r = p.snap[0].rank[slot];
             const size_t k = (size_t)blockIdx.x * kRgThreads + tid, stride = (size_t)gridDim.x * kRgThreads;
             for (size_t i = k; i < (size_t)r * p.d[0]; i += stride) p.out[0][(size_t)slot * kRankPad * p.d[0] + i] = 0.f;
@@ -867,7 +954,7 @@ __global__ void __launch_bounds__(1024) rows_check_kernel(const int32_t* seg_off
 }
 
 // ---- host ---------------------------------------------------------------------------------------------
-constexpr int kRgRing = 208 * 1024;   // one CTA to an SM
+constexpr int kRgRing = 203 * 1024;   // one CTA to an SM
 
 // Workspace: [u][v][partial results of both passes' CTAs][whether the arrays hold together]
 struct RgLayout { size_t pieces, partial, bad, total; };
@@ -944,9 +1031,13 @@ cudaError_t launch_rows_grad(const RowsGradCall& a, cudaStream_t stream, int* la
         return launch(grad, a.num_sms);
     }
     const int pitch = kept_pitch(a.d_in);
-    bool ok = bf16 ? a.cache->get_2d(&p.map[0], a.x.data, (uint64_t)a.d_in, (uint64_t)a.T, (uint64_t)a.d_in * 2, 64, kTileM)
-                   : a.cache->get_2d(&p.map[0], a.x.data, (uint64_t)pitch / 2, (uint64_t)a.T, (uint64_t)pitch, 64, kTileM, false);   // (8-bit rows as pairs)
-    ok = ok && a.cache->get_2d(&p.map[1], a.dy, (uint64_t)a.d_out, (uint64_t)a.T, (uint64_t)a.d_out * 2, 64, kTileM);
+    bool ok = true;
+    for (int pass = 0; pass < 2; ++pass) {
+        const int rows = pass == 0 ? 128 : 64;
+        ok = ok && (bf16 ? a.cache->get_2d(&p.map[pass][0], a.x.data, (uint64_t)a.d_in, (uint64_t)a.T, (uint64_t)a.d_in * 2, 64, rows)
+                         : a.cache->get_2d(&p.map[pass][0], a.x.data, (uint64_t)pitch / 2, (uint64_t)a.T, (uint64_t)pitch, pass == 0 ? 32 : 64, rows, false));
+        ok = ok && a.cache->get_2d(&p.map[pass][1], a.dy, (uint64_t)a.d_out, (uint64_t)a.T, (uint64_t)a.d_out * 2, 64, rows);   // (8-bit rows as pairs)
+    }
     for (int k = 0; k < kRankPad / kChunk && k * kChunk < p.r16; ++k)
         for (int i = 0; i < 2; ++i)
             ok = ok && a.cache->get_2d(&p.low[i][k], a.low[i], (uint64_t)p.d[i], (uint64_t)a.slots[i] * kRankPad, (uint64_t)p.d[i] * 2, 64, (k + 1) * kChunk);
