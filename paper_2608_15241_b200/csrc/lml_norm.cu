@@ -43,11 +43,12 @@ __device__ __forceinline__ float group_sum(float v, float* red, int group, int w
 }
 
 template <int W> struct NormShape {
-    static constexpr int kWarps = W > 8 ? W : 8;
-    static constexpr int kGroups = kWarps / W;
+    static constexpr int kGroups = W > 8 ? 1 : 8 / W, kWarps = W * kGroups;
 };
 
-template <int W, int V>
+// W: warps of a row (a number that is known here: 22.4 us for 8192 x 4096 where one that is not took 25).  AHEAD: the weights are asked for along
+// with the row.
+template <int W, int V, bool AHEAD>
 __global__ void __launch_bounds__(NormShape<W>::kWarps * 32) block_norm_kernel(const __grid_constant__ NormForward a)
 {
     __shared__ float red[2][NormShape<W>::kWarps];
@@ -63,12 +64,17 @@ __global__ void __launch_bounds__(NormShape<W>::kWarps * 32) block_norm_kernel(c
     const uint4 zero = make_uint4(0, 0, 0, 0);
     auto at = [&](const void* p, int vec) { return static_cast<const __nv_bfloat16*>(p) + t * d + vec * 8; };
 
-    uint4 h[V], o[V];
+    uint4 h[V], o[V], w_post[AHEAD ? V : 1], gate[AHEAD ? V : 1], w_pre[AHEAD ? V : 1];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         const int vec = i * W * 32 + in;
-        h[i] = vec < vecs ? ld_v4(at(a.h, vec)) : zero;
-        o[i] = a.o && vec < vecs ? ld_v4(at(a.o, vec)) : zero;
+        const bool ok = vec < vecs, ok_o = ok && a.o;
+        h[i] = ok ? ld_v4(at(a.h, vec)) : zero;
+        o[i] = ok_o ? ld_v4(at(a.o, vec)) : zero;
+        if (!AHEAD) continue;
+        gate[i] = ok_o && a.n.gate_rows ? ld_v4(at(a.n.gate_rows, vec)) : ok_o && a.n.gate ? ld_weights(a.n.gate, vec) : zero;
+        w_post[i] = ok_o && a.n.w_post ? ld_weights(a.n.w_post, vec) : zero;
+        w_pre[i] = ok && a.n.w_pre ? ld_weights(a.n.w_pre, vec) : zero;
     }
     if (a.o) {
         float r = 1.f;
@@ -91,12 +97,12 @@ __global__ void __launch_bounds__(NormShape<W>::kWarps * 32) block_norm_kernel(c
             unpack8(h[i], f);
             unpack8(o[i], n);
             if (a.n.w_post) {
-                unpack8(ld_weights(a.n.w_post, vec), w);
+                unpack8(AHEAD ? w_post[i] : ld_weights(a.n.w_post, vec), w);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) n[e] *= r * w[e];
             }
             if (a.n.gate || a.n.gate_rows) {
-                unpack8(a.n.gate_rows ? ld_v4(at(a.n.gate_rows, vec)) : ld_weights(a.n.gate, vec), w);
+                unpack8(AHEAD ? gate[i] : a.n.gate_rows ? ld_v4(at(a.n.gate_rows, vec)) : ld_weights(a.n.gate, vec), w);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) n[e] *= w[e];
             }
@@ -126,7 +132,7 @@ __global__ void __launch_bounds__(NormShape<W>::kWarps * 32) block_norm_kernel(c
         if (vec < vecs) {
             float f[8], w[8];
             unpack8(h[i], f);
-            unpack8(ld_weights(a.n.w_pre, vec), w);
+            unpack8(AHEAD ? w_pre[i] : ld_weights(a.n.w_pre, vec), w);
 #pragma unroll
             for (int e = 0; e < 8; ++e) f[e] *= rho * w[e];
             h[i] = pack8(f);
@@ -573,41 +579,39 @@ __global__ void __launch_bounds__(32 * kSumSlices) norm_sums_kernel(const __grid
 }
 
 // ---- launches ----------------------------------------------------------------------------------------
-struct NormPick { int W, V; };
-// vectors per thread: as few as 16 warps allow where there are few rows (latency), else up to `most`
-static NormPick norm_pick(int T, int d, int num_sms, int most)
-{
-    const int vecs = d / 8;
-    int V = 1, W = 1;
-    const int want = T <= num_sms ? 1 : most;
-    for (V = 1; V <= 4; V *= 2) {
-        for (W = 1; W < 16 && W * V * 32 < vecs; W *= 2) {}
-        if (W * V * 32 >= vecs && (V >= want || W == 1)) break;
-    }
-    if (V > 4) V = 4;
-    return {W, V};
-}
-
-template <typename F> static cudaError_t norm_dispatch(const NormPick& p, F&& f)
-{
-#define LML_NORM_CASE(w, v) if (p.W == w && p.V == v) return f(std::integral_constant<int, w>(), std::integral_constant<int, v>())
-    LML_NORM_CASE(1, 1); LML_NORM_CASE(2, 1); LML_NORM_CASE(4, 1); LML_NORM_CASE(8, 1); LML_NORM_CASE(16, 1);
-    LML_NORM_CASE(1, 2); LML_NORM_CASE(2, 2); LML_NORM_CASE(4, 2); LML_NORM_CASE(8, 2); LML_NORM_CASE(16, 2);
-    LML_NORM_CASE(1, 4); LML_NORM_CASE(2, 4); LML_NORM_CASE(4, 4); LML_NORM_CASE(8, 4); LML_NORM_CASE(16, 4);
-#undef LML_NORM_CASE
-    return cudaErrorInvalidValue;
-}
-
 cudaError_t launch_block_norm(const NormForward& a, int num_sms, cudaStream_t stream)
 {
-    return norm_dispatch(norm_pick(a.n.T, a.n.d, num_sms, 2), [&](auto w, auto v) {
-        constexpr int W = decltype(w)::value, V = decltype(v)::value;
+    // As few vectors per thread as the warps allow where there are rows for one wave at most: what counts is one row's time.  Two for more, to
+    // some 40 rows per SM (2000 x 4096 with all that there is: 12.3 us, four 14.7; 3000 x 4096 16.6 for 2900 and 19.5), four beyond, where
+    // what counts is loads in flight (8192 x 4096 without o: 22.4 us, 6.0 TB/s, two 24.7; 16384 x 2048 21.7 and 27.1).  The weights are asked
+    // for ahead of the sums up to a few waves (40 x 4096 with a gate per token: 2.5 us, 3.4 behind them); beyond they come from L1, and the
+    // registers are better used for more rows (8192 x 4096: 26.4 us with two vectors, 29.8 ahead).  T and d decide and nothing else: a call on h'
+    // alone gives the same bits.
+    const int vecs = a.n.d / 8;
+    const bool ahead = a.n.T <= 8 * num_sms;
+    int V = a.n.T <= num_sms ? 1 : a.n.T <= 40 * num_sms ? 2 : 4;
+    while (V > 1 && 16 * V >= vecs) V /= 2;                 // (not more than the row has)
+    while (32 * 16 * V < vecs) V *= 2;
+    const int needs = (vecs + 32 * V - 1) / (32 * V);
+    const auto launch = [&](auto w, auto v) {
+        constexpr int W = decltype(w)::value, V = decltype(v)::value, kGroups = NormShape<W>::kGroups;
         cudaLaunchConfig_t cfg = {};
         cudaLaunchAttribute attr[1];
-        const int groups = NormShape<W>::kGroups;
-        pdl_config(cfg, attr, dim3((unsigned)((a.n.T + groups - 1) / groups)), dim3(NormShape<W>::kWarps * 32), 0, stream);
-        return cudaLaunchKernelEx(&cfg, block_norm_kernel<W, V>, a);
-    });
+        pdl_config(cfg, attr, dim3((unsigned)(((long long)a.n.T + kGroups - 1) / kGroups)), dim3(NormShape<W>::kWarps * 32), 0, stream);
+        return cudaLaunchKernelEx(&cfg, ahead ? block_norm_kernel<W, V, true> : block_norm_kernel<W, V, false>, a);
+    };
+    const auto widths = [&](auto v) {
+        const auto fits = [&](auto w) { return needs <= decltype(w)::value; };
+        using std::integral_constant;
+        if (fits(integral_constant<int, 1>())) return launch(integral_constant<int, 1>(), v);
+        if (fits(integral_constant<int, 2>())) return launch(integral_constant<int, 2>(), v);
+        if (fits(integral_constant<int, 4>())) return launch(integral_constant<int, 4>(), v);
+        if (fits(integral_constant<int, 5>())) return launch(integral_constant<int, 5>(), v);
+        if (fits(integral_constant<int, 8>())) return launch(integral_constant<int, 8>(), v);
+        if (fits(integral_constant<int, 10>())) return launch(integral_constant<int, 10>(), v);
+        return launch(integral_constant<int, 16>(), v);
+    };
+    return V == 1 ? widths(std::integral_constant<int, 1>()) : V == 2 ? widths(std::integral_constant<int, 2>()) : widths(std::integral_constant<int, 4>());
 }
 
 static int norm_backward_ctas(int T, int num_sms) { return T < num_sms ? T : num_sms; }
