@@ -173,23 +173,7 @@ __device__ __forceinline__ void cp_async_word(uint32_t* dst, const uint32_t* src
 {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(ptx::smem_u32(dst)), "l"(src) : "memory");
 }
-// Pairs of fp32 values, and the eight values of a vector: packed as bf16, or as they are multiplied.
-__device__ __forceinline__ float2 fma2(const float2& x, const float2& y, const float2& z)
-{
-    float2 d;
-    asm("{.reg .b64 x, y, z, d;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n mov.b64 z, {%6, %7};\n"
-        " fma.rn.f32x2 d, x, y, z;\n mov.b64 {%0, %1}, d;}"
-        : "=f"(d.x), "=f"(d.y) : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y), "f"(z.x), "f"(z.y));
-    return d;
-}
-__device__ __forceinline__ float2 mul2(const float2& x, const float2& y)
-{
-    float2 d;
-    asm("{.reg .b64 x, y, d;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n mul.rn.f32x2 d, x, y;\n mov.b64 {%0, %1}, d;}"
-        : "=f"(d.x), "=f"(d.y) : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y));
-    return d;
-}
-__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+// The eight values of a vector: packed as bf16, or as they are multiplied.
 __device__ __forceinline__ void unpack_pairs(const uint4& v, float2 (&f)[4])
 {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -200,13 +184,6 @@ __device__ __forceinline__ uint4 pack_pairs(const float2 (&f)[4])
 {
     const float g[8] = {f[0].x, f[0].y, f[1].x, f[1].y, f[2].x, f[2].y, f[3].x, f[3].y};
     return pack8(g);
-}
-__device__ __forceinline__ float2 add2(const float2& x, const float2& y)
-{
-    float2 d;
-    asm("{.reg .b64 x, y, d;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n add.rn.f32x2 d, x, y;\n mov.b64 {%0, %1}, d;}"
-        : "=f"(d.x), "=f"(d.y) : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y));
-    return d;
 }
 template <bool PACKED> struct Eight;
 template <> struct Eight<true> {

@@ -44,32 +44,52 @@ __device__ __forceinline__ uint32_t byte_of_amax(uint32_t amax, bool e4m3)
 // have, so they become 240 units (1.875 * 2^127).
 constexpr uint32_t kTopByte = 247u;
 
+// Arithmetic on pairs of fp32 values.
+__device__ __forceinline__ float2 fma2(const float2& x, const float2& y, const float2& z)
+{
+    float2 d;
+    asm("{.reg .b64 x, y, z, d;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n mov.b64 z, {%6, %7};\n"
+        " fma.rn.f32x2 d, x, y, z;\n mov.b64 {%0, %1}, d;}"
+        : "=f"(d.x), "=f"(d.y) : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y), "f"(z.x), "f"(z.y));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(const float2& x, const float2& y)
+{
+    float2 d;
+    asm("{.reg .b64 x, y, d;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n mul.rn.f32x2 d, x, y;\n mov.b64 {%0, %1}, d;}"
+        : "=f"(d.x), "=f"(d.y) : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(const float2& x, const float2& y)
+{
+    float2 d;
+    asm("{.reg .b64 x, y, d;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n add.rn.f32x2 d, x, y;\n mov.b64 {%0, %1}, d;}"
+        : "=f"(d.x), "=f"(d.y) : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y));
+    return d;
+}
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
 // Eight consecutive values, packed bf16 -> 8 bits; byte: their block's scale byte.
 __device__ __forceinline__ uint2 encode8(const uint4& v, uint32_t byte, bool e4m3)
 {
-    const float inv = byte == 255u ? 0.f : __uint_as_float((254u - byte) << 23);   // 2^(127 - byte)
+    const float2 inv = both(byte == 255u ? 0.f : __uint_as_float((254u - byte) << 23));   // 2^(127 - byte)
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    uint32_t out[2];
+    uint32_t out[4];   // of two values each
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        float a = bf16_lo(w[2 * h]) * inv, b = bf16_hi(w[2 * h]) * inv, c = bf16_lo(w[2 * h + 1]) * inv, d = bf16_hi(w[2 * h + 1]) * inv;
+    for (int i = 0; i < 4; ++i) {
+        const float2 x = make_float2(bf16_lo(w[i]), bf16_hi(w[i]));
         if (e4m3) {
-            if (byte == kTopByte) {
-                a = fminf(fmaxf(a, -240.f), 240.f); b = fminf(fmaxf(b, -240.f), 240.f);
-                c = fminf(fmaxf(c, -240.f), 240.f); d = fminf(fmaxf(d, -240.f), 240.f);
-            }
-            const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
-            const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
-            out[h] = lo | hi << 16;
+            float2 q = mul2(x, inv);
+            if (byte == kTopByte) q = make_float2(fminf(fmaxf(q.x, -240.f), 240.f), fminf(fmaxf(q.y, -240.f), 240.f));
+            out[i] = __nv_cvt_float2_to_fp8x2(q, __NV_SATFINITE, __NV_E4M3);
         } else {
-            // rounding to an integer by adding 1.5 * 2^23: the low byte of the sum's bits is q in two's complement
-            const float m = 12582912.f;
-            const uint32_t qa = __float_as_uint(fminf(fmaxf(a, -127.f), 127.f) + m), qb = __float_as_uint(fminf(fmaxf(b, -127.f), 127.f) + m);
-            const uint32_t qc = __float_as_uint(fminf(fmaxf(c, -127.f), 127.f) + m), qd = __float_as_uint(fminf(fmaxf(d, -127.f), 127.f) + m);
-            out[h] = __byte_perm(__byte_perm(qa, qb, 0x0040), __byte_perm(qc, qd, 0x0040), 0x5410);
+            // rounding to an integer by adding 1.5 * 2^23: the low 16 bits of the sum's are q in two's complement (the product is exact)
+            const float2 q = fma2(x, inv, both(12582912.f));
+            out[i] = __vmins2(__vmaxs2(__byte_perm(__float_as_uint(q.x), __float_as_uint(q.y), 0x5410), 0xff81ff81u), 0x007f007fu);
         }
     }
-    return make_uint2(out[0], out[1]);
+    if (e4m3) return make_uint2(out[0] | out[1] << 16, out[2] | out[3] << 16);
+    return make_uint2(__byte_perm(out[0], out[1], 0x6420), __byte_perm(out[2], out[3], 0x6420));
 }
 __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
 {
