@@ -281,7 +281,8 @@ lml_status lora_mixed_linear_backward_adapters(lml_table* t, lml_table* t_T, con
  *   LML_ROWS_E4M3  q an FP8 E4M3 number, b the least with amax <= 448 * 2^(b - 127) (MXFP8): four significant bits.
  * Rounded to nearest even, off by half a step at most (E4M3: 3.3e38 and more become 3.19e38, the next would be 2^128).  b >= 0 (INT8), >= 3 (E4M3): blocks below about 2^-120 lose their
  * smallest values.  A block that holds Inf or NaN has b = 255 and reads back as NaN.
- * data:   uint8 [T][pitch], pitch = d rounded up to a multiple of 32, zeros behind column d.
+ * data:   uint8 [T][pitch], pitch = d rounded up to a multiple of 32, zeros behind column d.  (E4M3 codes 0x7f and 0xff, which the format has
+ *         for NaN and no store writes, stand for nothing: what is made of them is not specified.)
  * scales: uint8 [ceil(d / 128)][T][4]: b of the four blocks of 128 columns (0 for blocks behind the last).
  * Both are device memory of the caller's, 16-byte aligned, of lml_checkpoint_data_bytes(T, d) and
  * lml_checkpoint_scale_bytes(T, d) bytes (0 for invalid arguments).  LML_ROWS_BF16: data is bf16 [T][d], scales is NULL.
@@ -308,9 +309,10 @@ lml_status lml_checkpoint_load(int device, const lml_rows* kept, int T, int d, v
 /*
  * lora_mixed_linear_backward_adapters_rows — the adapter gradients with x kept as rows of any of the formats above.
  *   dA[slot][j][k] (+)= s sum_t (dy.B)[t][j] x[t][k],   dB[slot][n][j] (+)= s sum_t dy[t][n] (x.A^T)[t][j]
- * as in lora_mixed_linear_backward_adapters, with x the values that the rows stand for.  Two launches on the tensor cores; the two
- * small products are kept to 16 bits beyond the leading one instead of being rounded to bf16, so dA and dB carry fp32 sums of
- * products that are exact to about 2^-17.  The order of the sums is fixed by the sizes, the segments and the bindings: the same call gives the same bits.
+ * as in lora_mixed_linear_backward_adapters, with x the values that the rows stand for.  On the tensor cores; the two small products are
+ * fp32 and stay so on the way (three bf16 values each instead of one), so dA and dB are sums in fp32 of products that are not rounded.  The
+ * order of the sums is fixed by the sizes, the segments and the bindings: the same call gives the same bits.  Two launches for every 320
+ * segments (and one more where there are more than that); a call of no tokens has one.
  * accumulate != 0: rows j < rank of the slots in use are added to.  accumulate == 0: rows j < rank of EVERY live slot of t are
  * written, zeros where the batch has no token of it (a step's first micro-batch then needs no zeroed buffers).  Rows j >= rank
  * and slots without an adapter are left as they are either way.
@@ -318,6 +320,8 @@ lml_status lml_checkpoint_load(int device, const lml_rows* kept, int T, int d, v
  * rank adds nothing and sets LML_FLAG_BAD_SLOT (of t_T where t's slot is fine).  Malformed seg_offsets: LML_FLAG_BAD_OFFSETS,
  * nothing is added.  A token's Inf or NaN reaches the gradients of its own adapter only.
  * x, dy: rows in segment order (no perm), 16-byte aligned.  G >= 1.  dA, dB must not overlap x or dy.
+ * The CTAs that share an item count themselves in words of the table t: two calls on the SAME table must not overlap on the GPU, put
+ * them on one stream or order them.
  * workspace: device, 256-byte aligned, lml_backward_rows_workspace_bytes(t, T, G) bytes.  Errors: INVALID_ARG, WORKSPACE, CUDA.
  */
 size_t lml_backward_rows_workspace_bytes(const lml_table* t, int max_tokens, int max_segments);

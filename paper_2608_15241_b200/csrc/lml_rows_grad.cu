@@ -62,10 +62,10 @@ struct alignas(64) RowsGradParams {
     uint32_t* status[2];
     uint8_t* pieces[2];       // u, v
     float* partial;           // [CTA][2]: of the item that its part begins in, of the item that its part ends in
-    int* arrived;             // [CTA]: of the item that its part ends in and the next one goes on with; zero between calls
+    int* arrived[2];          // [CTA], of each pass: of the item that its part ends in and the next one goes on with; the other pass clears them
     float* out[2];            // dA, dB
     int d[2], tiles[2];       // d_in, d_out; in tiles of 128 columns
-    int T, G, r16, ring, accumulate, all_tiles, whole_items;
+    int T, G, num_sms, r16, ring, accumulate, all_tiles, whole_items;
     int check_first, check_last;   // the slice begins, ends the call
     unsigned long long live;  // slots with an adapter
 };
@@ -352,16 +352,12 @@ __device__ __forceinline__ RgShare share_of(const RgLine& line, int item, int n,
     return {first, line.part_of(item + n - 1), k == first ? 1 : 0};   // (the others begin behind the item's first step)
 }
 // After all finishing warps have written this CTA's partial result: if it is the last one of the item's, the CTA joins them later.
-__device__ __forceinline__ void arrive(RgCtrl* c, const RowsGradParams& p, const RgShare& s, int job, int slot, int at, int valid)
+__device__ __forceinline__ void arrive(RgCtrl* c, int* arrived, const RgShare& s, int job, int slot, int at, int valid)
 {
     __threadfence();
     finish_barrier();
     if (threadIdx.x == 64) {   // (the first of them)
-        const int n = atomicAdd(p.arrived + s.first, 1);
-        if (n == s.last - s.first) {
-            atomicExch(p.arrived + s.first, 0);   // (for the next call)
-            c->joins[c->n_joins++] = {job, slot, s.first, s.last, at, valid};
-        }
+        if (atomicAdd(arrived + s.first, 1) == s.last - s.first) c->joins[c->n_joins++] = {job, slot, s.first, s.last, at, valid};
         __threadfence();
     }
 }
@@ -471,6 +467,7 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_shrink_kernel(const __grid
     if (blockIdx.x == 0) {
         flag_segment(p, seg);
         if (bad && tid == 0) atomicOr(p.status[0], LML_FLAG_BAD_OFFSETS);
+        for (int i = tid; i < p.num_sms; i += kRgThreads) p.arrived[1][i] = 0;
     }
     const int mine = seg.mine && !bad ? (seg.s1 - seg.s0 + kTileM - 1) / kTileM : 0;
     int upto = mine;
@@ -594,7 +591,7 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_shrink_kernel(const __grid
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&c->acc_free[items & 1]));
-                if (!whole) arrive(c, p, share, t.job, t.slot, t.piece, t.valid);
+                if (!whole) arrive(c, p.arrived[0], share, t.job, t.slot, t.piece, t.valid);
             }
             fence_proxy_async_all();          // the pieces are read by bulk copies
         } else if (FMT != kBf16) {
@@ -892,7 +889,7 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_grad_kernel(const __grid_c
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&c->acc_free[items & 1]));
                 if (whole) continue;
-                arrive(c, p, share_of(line, t.item(), t.units, (int)blockIdx.x), job, t.slot, c0, 0);
+                arrive(c, p.arrived[1], share_of(line, t.item(), t.units, (int)blockIdx.x), job, t.slot, c0, 0);
             }
         } else {
             const int group = (warp - kRgFirstConv) / kRgGroup;
@@ -902,6 +899,8 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_grad_kernel(const __grid_c
     __syncwarp();
     if (*abort) __nanosleep(50000);
     grid_dependency_wait();   // (a CTA without units too: who waits for this grid has waited for the pieces' writers)
+    if (blockIdx.x == 0)
+        for (int i = tid; i < p.num_sms; i += kRgThreads) p.arrived[0][i] = 0;
     __syncthreads();
     for (int i = 0; i < c->n_joins; ++i) {
         const RgJoin s = c->joins[i];
@@ -1008,7 +1007,8 @@ cudaError_t launch_rows_grad(const RowsGradCall& a, cudaStream_t stream, int* la
     p.status[0] = a.status; p.status[1] = a.status_T;
     p.pieces[0] = ws; p.pieces[1] = ws + lay.pieces;
     p.partial = reinterpret_cast<float*>(ws + lay.partial);
-    p.arrived = a.arrived;
+    p.arrived[0] = a.arrived; p.arrived[1] = a.arrived + a.num_sms;
+    p.num_sms = a.num_sms;
     p.out[0] = a.dA; p.out[1] = a.dB;
     memset(p.map, 0, sizeof(p.map));
     memset(p.low, 0, sizeof(p.low));
