@@ -60,7 +60,6 @@ __global__ void __launch_bounds__(NormShape<W>::kWarps * 32) block_norm_kernel(c
     if (t >= T) return;   // (whole groups leave)
     float* red0 = red[0] + group * W;
     float* red1 = red[1] + group * W;
-    const float inv_d = 1.f / (float)d;
     const uint4 zero = make_uint4(0, 0, 0, 0);
     auto at = [&](const void* p, int vec) { return static_cast<const __nv_bfloat16*>(p) + t * d + vec * 8; };
 
@@ -87,7 +86,7 @@ __global__ void __launch_bounds__(NormShape<W>::kWarps * 32) block_norm_kernel(c
 #pragma unroll
                 for (int e = 0; e < 8; ++e) ss = fmaf(f[e], f[e], ss);
             }
-            r = rsqrtf(group_sum<W>(ss, red0, group, warp, lane) * inv_d + a.n.eps);
+            r = __frsqrt_rn(group_sum<W>(ss, red0, group, warp, lane) / (float)d + a.n.eps);
         }
 #pragma unroll
         for (int i = 0; i < V; ++i) {
@@ -125,7 +124,7 @@ __global__ void __launch_bounds__(NormShape<W>::kWarps * 32) block_norm_kernel(c
 #pragma unroll
         for (int e = 0; e < 8; ++e) ss = fmaf(f[e], f[e], ss);
     }
-    const float rho = rsqrtf(group_sum<W>(ss, red1, group, warp, lane) * inv_d + a.n.eps);
+    const float rho = __frsqrt_rn(group_sum<W>(ss, red1, group, warp, lane) / (float)d + a.n.eps);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         const int vec = i * W * 32 + in;

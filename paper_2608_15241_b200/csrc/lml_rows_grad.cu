@@ -50,6 +50,7 @@ constexpr int kRgMaxStages = 10;
 constexpr int kRgTurns = 16;                    // tiles on their way to and from the converting warps: as many as stages, and an end for each group
 static_assert(kRgTurns >= kRgMaxStages + kRgGroups && (kRgTurns & (kRgTurns - 1)) == 0, "a turn's place must have been read before it is used again");
 constexpr int kRgWords = 136;                   // scale words of half a step, one per row, brought in from a 16-byte boundary on (of 64 rows: 72)
+constexpr int kRgChunk = 8;                     // half steps that one accumulator takes; see issue_steps
 constexpr int kRgLeast = 4;                     // steps of a CTA's part (of a whole pass, if it has fewer)
 
 struct alignas(64) RowsGradParams {
@@ -117,6 +118,56 @@ __device__ __forceinline__ void tmem_ld_32x8(uint32_t taddr, uint32_t (&r)[8])
 {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st_32x8(uint32_t taddr, const float (&r)[8])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+                 :: "r"(__float_as_uint(r[0])), "r"(__float_as_uint(r[1])), "r"(__float_as_uint(r[2])), "r"(__float_as_uint(r[3])),
+                    "r"(__float_as_uint(r[4])), "r"(__float_as_uint(r[5])), "r"(__float_as_uint(r[6])), "r"(__float_as_uint(r[7])), "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// Eight columns of a chunk's accumulator (PARTS: the sums of three that stand r16 apart), plus, if `more`, of the sum of the chunks before at
+// `sum`.  By a whole warp.
+template <int PARTS>
+__device__ __forceinline__ void chunk_sums(uint32_t from, uint32_t r16, uint32_t sum, bool more, float (&s)[8])
+{
+    uint32_t h[8], m[8], l[8], before[8];
+    tmem_ld_32x8(from, h);
+    if (PARTS == 3) {
+        tmem_ld_32x8(from + r16, m);
+        tmem_ld_32x8(from + 2 * r16, l);
+    }
+    if (more) tmem_ld_32x8(sum, before);
+    tmem_ld_wait();
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        s[e] = __uint_as_float(h[e]);
+        if (PARTS == 3) s[e] += __uint_as_float(m[e]) + __uint_as_float(l[e]);
+        if (more) s[e] += __uint_as_float(before[e]);
+    }
+}
+// The chunks of an item but its last: waits for each in turn and adds it up at `sum`.  chunk: counted through the items of this CTA.
+template <int PARTS>
+__device__ __forceinline__ void sum_chunks(RgCtrl* c, uint32_t tmem, uint32_t acc_cols, uint32_t r16, uint32_t sum, int n, uint32_t& chunk, int lane, volatile int* abort)
+{
+    for (int k = 0; k + 1 < n; ++k, ++chunk) {
+        mbar_wait_warp(smem_u32(&c->acc_full[chunk & 1]), (chunk >> 1) & 1, abort);
+        __syncwarp();
+        tc_fence_after();
+#pragma unroll 1
+        for (uint32_t j = 0; j < r16; j += 8) {
+            float s[8];
+            chunk_sums<PARTS>(tmem + (chunk & 1) * acc_cols + j, r16, sum + j, k > 0, s);
+            tmem_st_32x8(sum + j, s);
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&c->acc_free[chunk & 1]));
+    }
+    mbar_wait_warp(smem_u32(&c->acc_full[chunk & 1]), (chunk >> 1) & 1, abort);
+    __syncwarp();
+    tc_fence_after();
 }
 __device__ __forceinline__ uint4 ld_smem_v4(uint32_t a)
 {
@@ -226,20 +277,22 @@ __device__ __forceinline__ void load_tile(RgCtrl* c, const CUtensorMap* map, uin
     if (SECOND && !raw) tma_load_2d(at + kRgHalfTile, map, bar, column + 64, row);
 }
 
-// Issuer of both passes: the steps as they come, told apart by what the producer says about them.  The tile's rows are the product's (first
+// Issuer of both passes: the steps as they come, told apart by what the producer says about them.  The tensor cores cut off what an addition to
+// an accumulator loses, always towards zero, so an item's sum goes through the accumulators in chunks of kRgChunk half steps, 32 additions, and
+// the finishing warps add those up, rounded, beside them in TMEM.  (Relative errors of dA and dB, 8192 x 11008 and 4096: <err> in one go.)  The tile's rows are the product's (first
 // pass: K-major) or contracted (second: M-major).
 template <bool SECOND>
 __device__ __forceinline__ void issue_steps(RgCtrl* c, const RgRing& ring, uint32_t tmem, uint32_t acc_cols, volatile int* abort)   // (one thread)
 {
     RgCursor u(ring);
-    uint32_t items = 0;
-    int flags;
+    uint32_t chunks = 0;   // begun
+    int flags, in_chunk = 0;
     do {
         if (!mbar_wait(smem_u32(&c->full[u.stage]), u.phase, abort)) return;
         const RgInfo info = c->info[u.stage];
         flags = info.flags;
-        const uint32_t buf = items & 1u, acc = tmem + buf * acc_cols, fresh = flags & kRgFirst ? 0u : 1u;
-        if (!fresh && items >= 2 && !mbar_wait(smem_u32(&c->acc_free[buf]), ((items >> 1) & 1u) ^ 1u, abort)) return;
+        const uint32_t buf = chunks & 1u, acc = tmem + buf * acc_cols, fresh = in_chunk == 0 ? 0u : 1u;
+        if (!fresh && chunks >= 2 && !mbar_wait(smem_u32(&c->acc_free[buf]), ((chunks >> 1) & 1u) ^ 1u, abort)) return;
         if (flags & kRgTouched) {
             if (!mbar_wait(smem_u32(&c->made[u.turn % kRgTurns]), turn_phase(u.turn), abort)) return;
             ++u.turn;
@@ -263,9 +316,10 @@ __device__ __forceinline__ void issue_steps(RgCtrl* c, const RgRing& ring, uint3
             for (int k = 0; k < 4; ++k) umma_bf16(acc, ad + (uint64_t)(k * 2), bd + (uint64_t)(k * 2), idesc, k > 0 ? 1u : fresh);
         }
         umma_commit(smem_u32(&c->empty[u.stage]));
-        if (flags & kRgLast) {
+        if (++in_chunk == kRgChunk || (flags & kRgLast)) {
             umma_commit(smem_u32(&c->acc_full[buf]));
-            ++items;
+            ++chunks;
+            in_chunk = 0;
         }
         u.advance();
     } while (!(flags & kRgEnd));
@@ -452,7 +506,7 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_shrink_kernel(const __grid
     RgCtrl* c = &ctrl;
     const uint32_t smem = (smem_u32(rg_smem) + 1023u) & ~1023u;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t cols = tmem_cols_for(2 * p.r16);
+    const uint32_t cols = tmem_cols_for(3 * p.r16);   // two accumulators, and the sum of the chunks before
     rg_setup(c, warp, tid, cols);
     // (After the allocation: what starts from here on may want TMEM and waits for this grid.  And after the wait: rows_grad_kernel
     // takes it that whatever came before this grid is complete.)
@@ -547,12 +601,11 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_shrink_kernel(const __grid
         } else if (warp < kRgOther) {
             // (After a wait that gave up these warps go through the rest all the same: the counters of shared items come out right.  The
             // status word says that the results do not.)
-            const int wt = tid - 64;
-            uint32_t items = 0;
-            for (ShrinkTasks t(p, c, w0, w1); t.next(); ++items) {
-                mbar_wait_warp(smem_u32(&c->acc_full[items & 1]), (items >> 1) & 1, abort);
-                __syncwarp();
-                tc_fence_after();
+            uint32_t chunk = 0;
+            const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), sum = lanes + 2 * p.r16;
+            for (ShrinkTasks t(p, c, w0, w1); t.next(); ++chunk) {
+                const int n_half = 2 * (t.n - 1) + halves((t.step + t.n - 1) * 128, p.d[t.job]), n_chunks = (n_half + kRgChunk - 1) / kRgChunk;
+                sum_chunks<1>(c, lanes, (uint32_t)p.r16, (uint32_t)(chunks_of_rank(p.snap[t.job].rank[t.slot]) * kChunk), sum, n_chunks, chunk, lane, abort);
                 // The products: lane = token.
                 const int r = p.snap[t.job].rank[t.slot], r16 = chunks_of_rank(r) * kChunk, row = (warp & 3) * 32 + lane;
                 const float sc = p.snap[t.job].scale[t.slot];
@@ -562,24 +615,23 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_shrink_kernel(const __grid
                 float* mine_at = p.partial + (size_t)(2 * blockIdx.x + share.slot) * kRgPartial;
                 // (r16 is a multiple of 16: the swizzle goes by j alone)
                 const bool there = row < t.valid;   // (rows behind the segment, columns behind the rank: whatever they hold)
-                const uint32_t from = tmem + (items & 1) * (uint32_t)p.r16 + ((uint32_t)((warp & 3) * 32) << 16);
+                const uint32_t from = lanes + (chunk & 1) * (uint32_t)p.r16;
                 // Two lanes share out two columns, so that each has both tokens of one: 4 bytes per store
                 const int odd = lane & 1;
                 uint8_t* const pair_at = out + (size_t)(row >> 6) * (r16 * 384) + (row & 6) * 2;
 #pragma unroll 1
                 for (int j = 0; j < r16; j += 8) {
-                    uint32_t v[8];
-                    tmem_ld_32x8(from + (uint32_t)j, v);
-                    tmem_ld_wait();
+                    float v[8];
+                    chunk_sums<1>(from + (uint32_t)j, 0, sum + (uint32_t)j, n_chunks > 1, v);
                     if (!whole) {
                         float* to = mine_at + j * 128 + row;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) to[e * 128] = __uint_as_float(v[e]);
+                        for (int e = 0; e < 8; ++e) to[e * 128] = v[e];
                         continue;
                     }
 #pragma unroll
                     for (int e = 0; e < 8; e += 2) {
-                        const float x = there && j + e < r ? __uint_as_float(v[e]) * sc : 0.f, y = there && j + e + 1 < r ? __uint_as_float(v[e + 1]) * sc : 0.f;
+                        const float x = there && j + e < r ? v[e] * sc : 0.f, y = there && j + e + 1 < r ? v[e + 1] * sc : 0.f;
                         const float got = __shfl_xor_sync(0xffffffffu, odd ? x : y, 1);
                         uint32_t part[3];
                         split3(odd ? got : x, odd ? y : got, part);
@@ -590,7 +642,7 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_shrink_kernel(const __grid
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&c->acc_free[items & 1]));
+                if (lane == 0) mbar_arrive(smem_u32(&c->acc_free[chunk & 1]));
                 if (!whole) arrive(c, p.arrived[0], share, t.job, t.slot, t.piece, t.valid);
             }
             fence_proxy_async_all();          // the pieces are read by bulk copies
@@ -710,7 +762,7 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_grad_kernel(const __grid_c
     RgCtrl* c = &ctrl;
     const uint32_t smem = (smem_u32(rg_smem) + 1023u) & ~1023u;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t cols = tmem_cols_for(6 * p.r16);
+    const uint32_t cols = tmem_cols_for(7 * p.r16);   // two accumulators of three parts, and the sum of the chunks before
     if (tid < kMaxSlots) c->units[tid] = 0;
     rg_setup(c, warp, tid, cols);
     grid_launch_dependents();   // (after the allocation, see rows_shrink_kernel)
@@ -805,12 +857,13 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_grad_kernel(const __grid_c
         } else if (warp == 1) {
             if (elect_one()) issue_steps<true>(c, ring, tmem, 3u * (uint32_t)p.r16, abort);
         } else if (warp < kRgOther) {
-            const int wt = tid - 64;   // (see rows_shrink_kernel)
-            uint32_t items = 0;
-            for (GradTasks t(p, c, w0, w1); t.next(); ++items) {
-                mbar_wait_warp(smem_u32(&c->acc_full[items & 1]), (items >> 1) & 1, abort);
-                __syncwarp();
-                tc_fence_after();
+            uint32_t chunk = 0;   // (see rows_shrink_kernel)
+            const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), sum = lanes + 6 * p.r16;
+            for (GradTasks t(p, c, w0, w1); t.next(); ++chunk) {
+                int n_half = 0;
+                for (RgPieces v(c, t); v.next();) n_half += halves(0, v.valid());
+                const int n_chunks = (n_half + kRgChunk - 1) / kRgChunk;
+                sum_chunks<3>(c, lanes, 3u * (uint32_t)p.r16, (uint32_t)(chunks_of_rank(p.snap[0].rank[t.slot]) * kChunk), sum, n_chunks, chunk, lane, abort);
                 // The sums, 16 columns of the accumulator at a time: lane = column of x or dy.  Partial results: dA [j][column], dB [column][j].
                 // dA is written as it stands, 128 bytes of a row per store; dB by way of shared memory, 64 bytes of a column's row.  (Four at a
                 // time straight to their places, each asked about: 205 us for the call where this took 176.)
@@ -821,19 +874,16 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_grad_kernel(const __grid_c
                 if (whole) dst = p.out[job] + (size_t)t.slot * kRankPad * d + (job == 0 ? c0 : c0 * kRankPad);
                 const int stride = !whole ? (job == 0 ? 128 : r16) : job == 0 ? d : kRankPad;   // between two j, or two columns
                 const int most = whole ? r : r16, columns = whole ? d - c0 : 128;               // of them that there are
-                const uint32_t from = tmem + (items & 1) * 3u * (uint32_t)p.r16 + ((uint32_t)col0 << 16);
+                const uint32_t from = lanes + (chunk & 1) * 3u * (uint32_t)p.r16;
 #pragma unroll 1
                 for (int j = 0; j < r16; j += 16) {
                     float s[16];
 #pragma unroll
                     for (int k = 0; k < 16; k += 8) {
-                        uint32_t h[8], m[8], l[8];
-                        tmem_ld_32x8(from + (uint32_t)(j + k), h);
-                        tmem_ld_32x8(from + (uint32_t)(r16 + j + k), m);
-                        tmem_ld_32x8(from + (uint32_t)(2 * r16 + j + k), l);
-                        tmem_ld_wait();
+                        float v[8];
+                        chunk_sums<3>(from + (uint32_t)(j + k), (uint32_t)r16, sum + (uint32_t)(j + k), n_chunks > 1, v);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) s[k + e] = __uint_as_float(h[e]) + (__uint_as_float(m[e]) + __uint_as_float(l[e]));
+                        for (int e = 0; e < 8; ++e) s[k + e] = v[e];
                     }
                     if (job == 0) {
                         float* to = dst + (size_t)j * stride + col0 + lane;
@@ -887,7 +937,7 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_grad_kernel(const __grid_c
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&c->acc_free[items & 1]));
+                if (lane == 0) mbar_arrive(smem_u32(&c->acc_free[chunk & 1]));
                 if (whole) continue;
                 arrive(c, p.arrived[1], share_of(line, t.item(), t.units, (int)blockIdx.x), job, t.slot, c0, 0);
             }
