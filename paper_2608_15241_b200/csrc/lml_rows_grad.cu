@@ -1107,7 +1107,7 @@ cudaError_t launch_rows_grad(const RowsGradCall& a, cudaStream_t stream, int* la
         p.check_first = g0 == 0; p.check_last = g0 + p.G == a.G;
         p.accumulate = a.accumulate || g0 > 0 ? 1 : 0;
         p.whole_items = 0;
-        const long long pieces = (a.T + kTileM - 1) / kTileM;
+        const long long pieces = a.T / kTileM + p.G;   // at most: every segment can have one that is not full
         cudaError_t e = launch(shrink, pieces * p.all_tiles / kRgLeast);
         if (e != cudaSuccess) return e;
         // Few pieces to an item: whole items, unless there are so many that their number leaves CTAs idle at the end.
