@@ -279,7 +279,8 @@ __device__ __forceinline__ void load_tile(RgCtrl* c, const CUtensorMap* map, uin
 
 // Issuer of both passes: the steps as they come, told apart by what the producer says about them.  The tensor cores cut off what an addition to
 // an accumulator loses, always towards zero, so an item's sum goes through the accumulators in chunks of kRgChunk half steps, 32 additions, and
-// the finishing warps add those up, rounded, beside them in TMEM.  (Relative errors of dA and dB, 8192 x 11008 and 4096: <err> in one go.)  The tile's rows are the product's (first
+// the finishing warps add those up, rounded, beside them in TMEM.  (Relative errors of dA and dB, 8192 x 11008 and 4096: 5.6e-7; 4.5e-6 in one go, 1.1e-6 with
+// twice as long chunks, which take the same time.)  The tile's rows are the product's (first
 // pass: K-major) or contracted (second: M-major).
 template <bool SECOND>
 __device__ __forceinline__ void issue_steps(RgCtrl* c, const RgRing& ring, uint32_t tmem, uint32_t acc_cols, volatile int* abort)   // (one thread)
@@ -754,6 +755,17 @@ struct RgPieces {
     __device__ size_t at() const { return (size_t)(at0 + k) * kRgPiece; }
 };
 
+// Half steps of a task: two for every piece, but for those that end a segment with no more than 64 rows.
+__device__ __forceinline__ int half_steps(const RgCtrl* c, const GradTasks& t)
+{
+    int n = 2 * (t.b - t.a);
+    for (int e = c->entry[t.slot];; ++e) {
+        const int len = c->len[e], end = c->pre[e] + (len + kTileM - 1) / kTileM;
+        if (end > t.a && end <= t.b && ((len - 1) & (kTileM - 1)) < 64) --n;
+        if (end >= t.b) return n;
+    }
+}
+
 template <int FMT>
 __global__ void __launch_bounds__(kRgThreads, 1) rows_grad_kernel(const __grid_constant__ RowsGradParams p)
 {
@@ -860,9 +872,7 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_grad_kernel(const __grid_c
             uint32_t chunk = 0;   // (see rows_shrink_kernel)
             const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), sum = lanes + 6 * p.r16;
             for (GradTasks t(p, c, w0, w1); t.next(); ++chunk) {
-                int n_half = 0;
-                for (RgPieces v(c, t); v.next();) n_half += halves(0, v.valid());
-                const int n_chunks = (n_half + kRgChunk - 1) / kRgChunk;
+                const int n_chunks = (half_steps(c, t) + kRgChunk - 1) / kRgChunk;
                 sum_chunks<3>(c, lanes, 3u * (uint32_t)p.r16, (uint32_t)(chunks_of_rank(p.snap[0].rank[t.slot]) * kChunk), sum, n_chunks, chunk, lane, abort);
                 // The sums, 16 columns of the accumulator at a time: lane = column of x or dy.  Partial results: dA [j][column], dB [column][j].
                 // dA is written as it stands, 128 bytes of a row per store; dB by way of shared memory, 64 bytes of a column's row.  (Four at a
