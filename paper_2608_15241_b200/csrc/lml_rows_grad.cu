@@ -15,7 +15,7 @@
 //
 // Both are rings of tiles of x or dy as TMA brings them in, multiplied by tcgen05 into one of two accumulators.  Roles: three producers, of
 // tiles, of the other operand and of scale words (one thread for two of them is the slowest role: a copy costs it a few hundred cycles), the
-// second of which tells the others what a stage holds; an issuer; four warps that finish items while the next one is multiplied;
+// first of which tells the others what a stage holds; an issuer; four warps that finish items while the next one is multiplied;
 // groups of warps that take 8-bit tiles in turn through their registers and write them beside as bf16 (exact: the
 // scales are powers of two) in the swizzled order of the tensor cores.  The second product contracts over tokens: the tile
 // [token][64 columns] is an operand whose contiguous index is the output's (M-major), which the descriptor says; nothing is
@@ -86,7 +86,7 @@ struct RgTurn { int stage, phase; };   // stage < 0: no more
 struct RgJoin { int job, slot, first, last, at, valid; };   // at: piece (first pass), column (second)
 
 struct RgCtrl {
-    unsigned long long full[kRgMaxStages], empty[kRgMaxStages], turn[kRgTurns], made[kRgTurns], acc_full[2], acc_free[2];
+    unsigned long long full[kRgMaxStages], low_full[kRgMaxStages], empty[kRgMaxStages], turn[kRgTurns], made[kRgTurns], acc_full[2], acc_free[2];
     RgInfo info[kRgMaxStages];
     RgTurn turns[kRgTurns];
     uint32_t used_half[2];   // slots in use
@@ -200,7 +200,8 @@ __device__ __forceinline__ void rg_setup(RgCtrl* c, int warp, int tid, uint32_t 
         c->n_joins = 0;
         c->used_half[0] = c->used_half[1] = 0u;
         for (int i = 0; i < kRgMaxStages; ++i) {
-            mbar_init(smem_u32(&c->full[i]), 3);
+            mbar_init(smem_u32(&c->full[i]), 2);       // (tile and words: all that the converting warps wait for)
+            mbar_init(smem_u32(&c->low_full[i]), 1);
             mbar_init(smem_u32(&c->empty[i]), 1);
         }
         for (int i = 0; i < kRgTurns; ++i) {
@@ -252,13 +253,18 @@ __device__ __forceinline__ void post_turn(RgCtrl* c, int turn, int stage, uint32
     mbar_arrive(smem_u32(&c->turn[turn % kRgTurns]));   // (releases what was written)
 }
 // ... the words of half a step's rows into the stage, from `words` on.  A bulk copy wants 16-byte boundaries, so it begins up to three words
-// early, and takes so many more; where that would reach behind the array's end, ordinary loads bring the rest.
+// early, and takes so many more; where that would reach behind the array's end (`last`), ordinary loads bring the rest.
 template <bool SECOND>
-__device__ __forceinline__ void load_words(RgCtrl* c, int stage, const uint32_t* words, const uint32_t* words_end)
+__device__ __forceinline__ void load_words(RgCtrl* c, int stage, const uint32_t* words, bool last, const uint32_t* words_end)
 {
     constexpr int kWords = SECOND ? 72 : kRgWords;
     const uint32_t bar = smem_u32(&c->full[stage]);
     const uint32_t* from = reinterpret_cast<const uint32_t*>(reinterpret_cast<uintptr_t>(words) & ~(uintptr_t)15);
+    if (!last) {
+        mbar_arrive_expect_tx(bar, kWords * 4);
+        bulk_load(smem_u32(c->words[stage]), from, kWords * 4, bar);
+        return;
+    }
     uint32_t bytes = kWords * 4;
     if (words_end - from < kWords) {
         bytes = (uint32_t)(words_end - from) * 4u & ~15u;
@@ -298,6 +304,7 @@ __device__ __forceinline__ void issue_steps(RgCtrl* c, const RgRing& ring, uint3
             if (!mbar_wait(smem_u32(&c->made[u.turn % kRgTurns]), turn_phase(u.turn), abort)) return;
             ++u.turn;
         }
+        if (!mbar_wait(smem_u32(&c->low_full[u.stage]), u.phase, abort)) return;
         tc_fence_after();
         const uint32_t low = u.at + ring.low;
         const uint64_t bd = umma_desc_k128(low);
@@ -545,17 +552,19 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_shrink_kernel(const __grid
     const int w0 = line.begin((int)blockIdx.x), w1 = line.begin((int)blockIdx.x + 1);
 
     const RgRing ring(smem, p.ring, FMT != kBf16, (uint32_t)p.r16 * 128u);
-    // Every half step of this CTA, for a producer: wait for its stage, then `f`.
-    auto each = [&](auto&& f) {
+    // Every half step of this CTA, for a producer: wait for its stage, then `f`.  `item`: what it keeps for an item's.
+    auto each = [&](auto&& item, auto&& f) {
         RgCursor u(ring);
         for (ShrinkTasks t(p, c, w0, w1); t.next();) {
+            const int d = p.d[t.job];
             const bool end = t.w + t.n == w1;
+            item(t);
             int k = t.step * 128;
             for (int left = t.n; left > 0; --left, k += 128) {
-                const int n = halves(k, p.d[t.job]);
+                const int n = halves(k, d);
                 for (int half = 0; half < n; ++half, u.advance()) {
                     if (!mbar_wait(smem_u32(&c->empty[u.stage]), u.phase ^ 1u, abort)) return u.turn;
-                    f(u, t, k, half, left == 1 && half + 1 == n, end);
+                    f(u, k, half, left == 1 && half + 1 == n ? end ? kRgLast | kRgEnd : kRgLast : 0);
                 }
             }
         }
@@ -563,37 +572,59 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_shrink_kernel(const __grid
     };
     if (w0 < w1) {
         if (warp == 0) {
-            if (elect_one())
-                each([&](RgCursor& u, const ShrinkTasks& t, int k, int half, bool, bool) {
-                    load_tile<false>(c, &p.map[0][t.job], u.at, u.stage, FMT != kBf16 && t.job == 0, t.row, k + 64 * half);
-                });
+            if (elect_one()) {
+                const CUtensorMap* map = nullptr;
+                bool raw = false, first = false;
+                int r16 = 0, valid = 0, row = 0;
+                uint32_t words_at = 0;   // in words of four bytes; what counts is where they lie to 16
+                each([&](const ShrinkTasks& t) {
+                         map = &p.map[0][t.job]; row = t.row; valid = t.valid;
+                         r16 = chunks_of_rank(p.snap[t.job].rank[t.slot]) * kChunk;
+                         raw = FMT != kBf16 && t.job == 0; first = true;
+                         words_at = (uint32_t)(reinterpret_cast<uintptr_t>(p.scales) >> 2) + (uint32_t)t.row;
+                     },
+                     [&](RgCursor& u, int k, int half, int last) {
+                         const int flags = last | (raw ? kRgTouched : 0) | (first ? kRgFirst : 0) | (half ? kRgRight : 0);
+                         first = false;
+                         c->info[u.stage] = {flags, valid, r16, raw ? (int)((words_at + (uint32_t)(k >> 7) * (uint32_t)p.T) & 3u) : -1};
+                         load_tile<false>(c, map, u.at, u.stage, raw, row, k + 64 * half);
+                     });
+            }
         } else if (warp == kRgOther) {
-            if (elect_one())
-                each([&](RgCursor& u, const ShrinkTasks& t, int k, int half, bool last, bool end) {
-                    const int chunks = chunks_of_rank(p.snap[t.job].rank[t.slot]);
-                    const bool raw = FMT != kBf16 && t.job == 0;
-                    int flags = raw ? kRgTouched : 0;
-                    if (half) flags |= kRgRight;
-                    else if (k == t.step * 128) flags |= kRgFirst;
-                    if (last) flags |= end ? kRgLast | kRgEnd : kRgLast;
-                    c->info[u.stage] = {flags, t.valid, chunks * kChunk,
-                                        raw ? (int)(reinterpret_cast<uintptr_t>(p.scales + (size_t)(k >> 7) * p.T + t.row) >> 2) & 3 : -1};
-                    const uint32_t bar = smem_u32(&c->full[u.stage]);
-                    mbar_arrive_expect_tx(bar, (uint32_t)chunks * (kChunk * 128u));
-                    tma_load_2d(u.at + ring.low, &p.low[t.job][chunks - 1], bar, k + 64 * half, t.slot * kRankPad);
-                });
+            if (elect_one()) {
+                const CUtensorMap* map = nullptr;
+                uint32_t bytes = 0;
+                int row = 0;
+                each([&](const ShrinkTasks& t) {
+                         const int chunks = chunks_of_rank(p.snap[t.job].rank[t.slot]);
+                         map = &p.low[t.job][chunks - 1]; bytes = (uint32_t)chunks * (kChunk * 128u); row = t.slot * kRankPad;
+                     },
+                     [&](RgCursor& u, int k, int half, int) {
+                         const uint32_t bar = smem_u32(&c->low_full[u.stage]);
+                         mbar_arrive_expect_tx(bar, bytes);
+                         tma_load_2d(u.at + ring.low, map, bar, k + 64 * half, row);
+                     });
+            }
         } else if (warp == kRgWordsWarp) {
             if (elect_one()) {
-                const uint32_t* words_end = p.scales + (size_t)kept_groups(p.d[0]) * p.T;
-                const int turns = each([&](RgCursor& u, const ShrinkTasks& t, int k, int, bool, bool) {
-                    if (FMT == kBf16 || t.job) {
-                        mbar_arrive(smem_u32(&c->full[u.stage]));
-                    } else {
-                        load_words<false>(c, u.stage, p.scales + (size_t)(k >> 7) * p.T + t.row, words_end);
-                        post_turn(c, u.turn, u.stage, u.phase);
-                        ++u.turn;
-                    }
-                });
+                const uint32_t *words = nullptr, *words_end = p.scales + (size_t)kept_groups(p.d[0]) * p.T;
+                bool raw = false;
+                bool last = false;
+                const int turns = each([&](const ShrinkTasks& t) {
+                        raw = FMT != kBf16 && t.job == 0;
+                        words = p.scales + t.row + (size_t)t.step * p.T;
+                        last = t.step + t.n == p.tiles[0];
+                    },
+                    [&](RgCursor& u, int, int half, int) {
+                        if (!raw) {
+                            mbar_arrive(smem_u32(&c->full[u.stage]));
+                        } else {
+                            load_words<false>(c, u.stage, words, last, words_end);
+                            if (half) words += p.T;   // (a step with one half is the last)
+                            post_turn(c, u.turn, u.stage, u.phase);
+                            ++u.turn;
+                        }
+                    });
                 if (FMT != kBf16)
                     for (int k = 0; k < kRgGroups; ++k) post_turn(c, turns + k, -1, 0);
             }
@@ -816,21 +847,20 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_grad_kernel(const __grid_c
     const int w0 = p.whole_items ? (int)blockIdx.x : line.begin((int)blockIdx.x), w1 = p.whole_items ? line.W : line.begin((int)blockIdx.x + 1);
 
     const RgRing ring(smem, p.ring, FMT != kBf16, (uint32_t)p.r16 * 384u);
-    auto each = [&](auto&& f) {   // (see rows_shrink_kernel)
+    auto each = [&](auto&& item, auto&& f) {   // (see rows_shrink_kernel)
         RgCursor u(ring);
         for (GradTasks t(p, c, w0, w1); t.next();) {
             const bool raw = FMT != kBf16 && t.job() == 0, end = t.last();
-            bool first = true;
+            int first = kRgFirst;
+            item(t, raw);
             for (RgPieces v(c, t); v.next();) {
                 const int valid = v.valid(), n = halves(0, valid);
                 for (int half = 0; half < n; ++half, u.advance()) {
                     if (!mbar_wait(smem_u32(&c->empty[u.stage]), u.phase ^ 1u, abort)) return u.turn;
                     const int rows = min(valid - 64 * half, 64);
-                    int flags = raw || (rows & 15) ? kRgTouched : 0;
-                    if (first) flags |= kRgFirst;
-                    first = false;
-                    if (v.left == 0 && half + 1 == n) flags |= end ? kRgLast | kRgEnd : kRgLast;
-                    f(u, t, v, raw, half, rows, flags);
+                    const int flags = first | (raw || (rows & 15) ? kRgTouched : 0) | (v.left == 0 && half + 1 == n ? end ? kRgLast | kRgEnd : kRgLast : 0);
+                    first = 0;
+                    f(u, v, half, rows, flags);
                 }
             }
         }
@@ -838,32 +868,47 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_grad_kernel(const __grid_c
     };
     if (w0 < w1) {
         if (warp == 0) {
-            if (elect_one())
-                each([&](RgCursor& u, const GradTasks& t, const RgPieces& v, bool raw, int half, int, int) {
-                    load_tile<true>(c, &p.map[1][t.job()], u.at, u.stage, raw, v.row() + 64 * half, t.column());
-                });
+            if (elect_one()) {
+                const CUtensorMap* map = nullptr;
+                bool is_raw = false;
+                int column = 0, r16 = 0;
+                uint32_t words_at = 0;
+                each([&](const GradTasks& t, bool raw) {
+                         map = &p.map[1][t.job()]; is_raw = raw; column = t.column();
+                         r16 = chunks_of_rank(p.snap[0].rank[t.slot]) * kChunk;
+                         words_at = (uint32_t)(reinterpret_cast<uintptr_t>(p.scales) >> 2) + (uint32_t)t.tile * (uint32_t)p.T;
+                     },
+                     [&](RgCursor& u, const RgPieces& v, int half, int rows, int flags) {
+                         c->info[u.stage] = {flags, rows, r16, is_raw ? (int)((words_at + (uint32_t)v.row()) & 3u) : -1};   // (64 rows on it is the same)
+                         load_tile<true>(c, map, u.at, u.stage, is_raw, v.row() + 64 * half, column);
+                     });
+            }
         } else if (warp == kRgOther) {
             if (elect_one()) {
                 grid_dependency_wait();   // (the tiles are on their way meanwhile)
                 fence_proxy_async_all();
-                each([&](RgCursor& u, const GradTasks& t, const RgPieces& v, bool raw, int half, int rows, int flags) {
-                    const int r16 = chunks_of_rank(p.snap[0].rank[t.slot]) * kChunk;
-                    const uint32_t low = (uint32_t)r16 * 384u;
-                    c->info[u.stage] = {flags, rows, r16,
-                                        raw ? (int)(reinterpret_cast<uintptr_t>(p.scales + (size_t)t.tile * p.T + v.row()) >> 2) & 3 : -1};
-                    const uint32_t bar = smem_u32(&c->full[u.stage]);
-                    mbar_arrive_expect_tx(bar, low);
-                    bulk_load(u.at + ring.low, p.pieces[t.job() ^ 1] + v.at() + half * low, low, bar);   // (u for dy, v for x)
-                });
+                uint32_t low = 0;
+                const uint8_t* pieces = nullptr;
+                each([&](const GradTasks& t, bool) {
+                         low = (uint32_t)(chunks_of_rank(p.snap[0].rank[t.slot]) * kChunk) * 384u;
+                         pieces = p.pieces[t.job() ^ 1];   // (u for dy, v for x)
+                     },
+                     [&](RgCursor& u, const RgPieces& v, int half, int, int) {
+                         const uint32_t bar = smem_u32(&c->low_full[u.stage]);
+                         mbar_arrive_expect_tx(bar, low);
+                         bulk_load(u.at + ring.low, pieces + v.at() + half * low, low, bar);
+                     });
             }
         } else if (warp == kRgWordsWarp) {
             if (elect_one()) {
-                const uint32_t* words_end = p.scales + (size_t)kept_groups(p.d[0]) * p.T;
-                const int turns = each([&](RgCursor& u, const GradTasks& t, const RgPieces& v, bool raw, int half, int, int flags) {
-                    if (raw) load_words<true>(c, u.stage, p.scales + (size_t)t.tile * p.T + v.row() + 64 * half, words_end);
-                    else mbar_arrive(smem_u32(&c->full[u.stage]));
-                    if (flags & kRgTouched) { post_turn(c, u.turn, u.stage, u.phase); ++u.turn; }
-                });
+                const uint32_t *words = nullptr, *words_end = p.scales + (size_t)kept_groups(p.d[0]) * p.T;
+                bool is_raw = false, last = false;
+                const int turns = each([&](const GradTasks& t, bool raw) { is_raw = raw; words = p.scales + (size_t)t.tile * p.T; last = t.tile + 1 == p.tiles[0]; },
+                    [&](RgCursor& u, const RgPieces& v, int half, int, int flags) {
+                        if (is_raw) load_words<true>(c, u.stage, words + v.row() + 64 * half, last, words_end);
+                        else mbar_arrive(smem_u32(&c->full[u.stage]));
+                        if (flags & kRgTouched) { post_turn(c, u.turn, u.stage, u.phase); ++u.turn; }
+                    });
                 for (int k = 0; k < kRgGroups; ++k) post_turn(c, turns + k, -1, 0);
             }
         } else if (warp == 1) {
