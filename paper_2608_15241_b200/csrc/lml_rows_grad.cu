@@ -7,7 +7,8 @@
 // rows_grad_kernel: dA and dB.  An item is (slot, 128 columns of x or dy), its work the slot's pieces.
 // A step of either is a tile of 128 rows x 128 columns, which goes through the rings in two halves along what is contracted: 64 columns in the
 // first pass, 64 rows in the second: a stage's way through loading, conversion and product is some 4000 cycles whatever its size, so
-// what counts is how many there are (three stages for the six and four that fit beside 64 ranks: 240 us for 180).
+// what counts is how many there are (beside 64 ranks eight and five, 145 us for 8192 x 11008 in E4M3 and 4096; with the 8 bits in a place of
+// their own six and four, 153).
 // In both the work of all items stands in one line that is cut into equal parts, one per SM; a CTA walks its part without a pause
 // between items.  An item that the cuts divide is joined in device memory: every CTA writes its partial result, and the last one to
 // arrive adds them in the order of the parts, so the bits do not depend on who that is.  (A form with a cluster per item and an
@@ -16,7 +17,7 @@
 // Both are rings of tiles of x or dy as TMA brings them in, multiplied by tcgen05 into one of two accumulators.  Roles: three producers, of
 // tiles, of the other operand and of scale words (one thread for two of them is the slowest role: a copy costs it a few hundred cycles), the
 // first of which tells the others what a stage holds; an issuer; four warps that finish items while the next one is multiplied;
-// groups of warps that take 8-bit tiles in turn through their registers and write them beside as bf16 (exact: the
+// groups of warps that take 8-bit tiles in turn through their registers and write them back in place as bf16 (exact: the
 // scales are powers of two) in the swizzled order of the tensor cores.  The second product contracts over tokens: the tile
 // [token][64 columns] is an operand whose contiguous index is the output's (M-major), which the descriptor says; nothing is
 // transposed.
@@ -186,6 +187,15 @@ __device__ __forceinline__ float4 ld_cg_v4(const float* p)   // (written by anot
     return v;
 }
 __device__ __forceinline__ void finish_barrier() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kRgFinish) : "memory"); }
+// Of a converting group; whether any thread says so.
+__device__ __forceinline__ bool group_any(int group, bool v)
+{
+    int r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.s32 p, %1, 0;\n\tbar.red.or.pred q, %2, %3, p;\n\tselp.s32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"(v ? 1 : 0), "r"(2 + group), "n"(32 * kRgGroup) : "memory");
+    return r != 0;
+}
+
 // Whether a segment's two bindings name one adapter in both tables.
 __device__ __forceinline__ bool paired(const RowsGradParams& p, int s, int sT)
 {
@@ -221,16 +231,12 @@ __device__ __forceinline__ void rg_setup(RgCtrl* c, int warp, int tid, uint32_t 
 }
 __device__ __forceinline__ uint32_t tmem_cols_for(int n) { return n <= 32 ? 32u : n <= 64 ? 64u : n <= 128 ? 128u : n <= 256 ? 256u : 512u; }
 
-// The ring of a CTA: stages of a tile as it is multiplied, beside it its 8 bits (if it has any), then the other operand (of the widest
-// adapter).  Every role walks it with a cursor of its own (a division per step to find the stage costs as much as the step's products).
+// The ring of a CTA: stages of a tile beside the other operand (of the widest adapter).  A tile's 8 bits come into its second half.  Every role walks
+// it with a cursor of its own (a division per step to find the stage costs as much as the step's products).
 struct RgRing {
-    uint32_t base, stage_bytes, low;
+    uint32_t base, stage_bytes;
     int stages;
-    __device__ RgRing(uint32_t at, int bytes, bool raw, uint32_t low_bytes) : base(at), low(kRgTile + (raw ? kRgRaw : 0))
-    {
-        stage_bytes = low + low_bytes;
-        stages = min(bytes / (int)stage_bytes, kRgMaxStages);
-    }
+    __device__ RgRing(uint32_t at, int bytes, uint32_t low) : base(at), stage_bytes(kRgTile + low), stages(min(bytes / (int)(kRgTile + low), kRgMaxStages)) {}
 };
 struct RgCursor {
     const RgRing& ring;
@@ -279,7 +285,7 @@ __device__ __forceinline__ void load_tile(RgCtrl* c, const CUtensorMap* map, uin
 {
     const uint32_t bar = smem_u32(&c->full[stage]);
     mbar_arrive_expect_tx(bar, raw ? kRgRaw : kRgTile);
-    tma_load_2d(raw ? at + kRgTile : at, map, bar, raw ? column / 2 : column, row);   // (8-bit columns in pairs)
+    tma_load_2d(raw ? at + (kRgTile - kRgRaw) : at, map, bar, raw ? column / 2 : column, row);   // (8-bit columns in pairs)
     if (SECOND && !raw) tma_load_2d(at + kRgHalfTile, map, bar, column + 64, row);
 }
 
@@ -306,7 +312,7 @@ __device__ __forceinline__ void issue_steps(RgCtrl* c, const RgRing& ring, uint3
         }
         if (!mbar_wait(smem_u32(&c->low_full[u.stage]), u.phase, abort)) return;
         tc_fence_after();
-        const uint32_t low = u.at + ring.low;
+        const uint32_t low = u.at + kRgTile;
         const uint64_t bd = umma_desc_k128(low);
         if (SECOND) {
             const uint32_t idesc = umma_idesc_bf16(128, 3 * info.r16) | kIdescMMajorA;
@@ -349,7 +355,7 @@ __device__ __forceinline__ void convert_tiles(RgCtrl* c, const RgRing& ring, int
         bool ok = mbar_wait_warp(smem_u32(&c->turn[k]), turn_phase(turn), abort);
         __syncwarp();
         const RgTurn what = c->turns[k];
-        if (ok && what.stage < 0) return;
+        ok = ok && what.stage >= 0;
         const int stage = what.stage < 0 ? 0 : what.stage;
         ok = ok && mbar_wait_warp(smem_u32(&c->full[stage]), (uint32_t)what.phase, abort);
         __syncwarp();
@@ -360,14 +366,14 @@ __device__ __forceinline__ void convert_tiles(RgCtrl* c, const RgRing& ring, int
         uint32_t byte[kParts], most = 0;
 #pragma unroll
         for (int q = 0; q < kParts; ++q) {
-            const uint4 w = ld_smem_v4(at + (uint32_t)(kRgTile + q * (kRgRaw / kParts) + wt * 16));
+            const uint4 w = ld_smem_v4(at + (uint32_t)(kRgTile - kRgRaw + q * (kRgRaw / kParts) + wt * 16));
             v[q][0] = odd ? make_uint2(w.z, w.w) : make_uint2(w.x, w.y);
             v[q][1] = odd ? make_uint2(w.x, w.y) : make_uint2(w.z, w.w);
             byte[q] = (c->words[stage][(info.word & 3) + row0 + kRows * q] >> shift) & 0xffu;
             most = max(most, byte[q]);
         }
         const bool usual = (!SECOND || info.valid == 64) && most <= Decoder<E4M3>::kMost;
-        if (!ok) return;   // (a wait gave up)
+        if (group_any(group, !ok)) return;   // (everybody has the tile's values, so their place may be written; or there is no more, or a wait gave up)
         const uint32_t to = at + to0;
         if (info.word >= 0 && usual) {
 #pragma unroll
@@ -551,7 +557,7 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_shrink_kernel(const __grid
     const RgLine line(c->pre[kRgSegs] * (p.tiles[0] + p.tiles[1]));
     const int w0 = line.begin((int)blockIdx.x), w1 = line.begin((int)blockIdx.x + 1);
 
-    const RgRing ring(smem, p.ring, FMT != kBf16, (uint32_t)p.r16 * 128u);
+    const RgRing ring(smem, p.ring, (uint32_t)p.r16 * 128u);
     // Every half step of this CTA, for a producer: wait for its stage, then `f`.  `item`: what it keeps for an item's.
     auto each = [&](auto&& item, auto&& f) {
         RgCursor u(ring);
@@ -602,7 +608,7 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_shrink_kernel(const __grid
                      [&](RgCursor& u, int k, int half, int) {
                          const uint32_t bar = smem_u32(&c->low_full[u.stage]);
                          mbar_arrive_expect_tx(bar, bytes);
-                         tma_load_2d(u.at + ring.low, map, bar, k + 64 * half, row);
+                         tma_load_2d(u.at + kRgTile, map, bar, k + 64 * half, row);
                      });
             }
         } else if (warp == kRgWordsWarp) {
@@ -846,7 +852,7 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_grad_kernel(const __grid_c
     const RgLine line(total * p.all_tiles);
     const int w0 = p.whole_items ? (int)blockIdx.x : line.begin((int)blockIdx.x), w1 = p.whole_items ? line.W : line.begin((int)blockIdx.x + 1);
 
-    const RgRing ring(smem, p.ring, FMT != kBf16, (uint32_t)p.r16 * 384u);
+    const RgRing ring(smem, p.ring, (uint32_t)p.r16 * 384u);
     auto each = [&](auto&& item, auto&& f) {   // (see rows_shrink_kernel)
         RgCursor u(ring);
         for (GradTasks t(p, c, w0, w1); t.next();) {
@@ -896,7 +902,7 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_grad_kernel(const __grid_c
                      [&](RgCursor& u, const RgPieces& v, int half, int, int) {
                          const uint32_t bar = smem_u32(&c->low_full[u.stage]);
                          mbar_arrive_expect_tx(bar, low);
-                         bulk_load(u.at + ring.low, pieces + v.at() + half * low, low, bar);
+                         bulk_load(u.at + kRgTile, pieces + v.at() + half * low, low, bar);
                      });
             }
         } else if (warp == kRgWordsWarp) {
