@@ -117,6 +117,19 @@ def test_backward(T, d, gate, post, form):
             assert (got[k] == 0.25).all(), name
 
 
+# More rows than a wave: two and four vectors per thread; the rings of the backward pass gone round many times, by one and by several groups of
+# warps, of one stage (the widest row of all inputs), and by the kernels of the usual call, whose threads' columns make up the row.
+@pytest.mark.parametrize("T,d", [(1300, 264), (2000, 2560), (6100, 264), (6100, 1032), (6100, 8)])
+def test_forward_of_many_rows(T, d):
+    test_forward(T, d, "shared", True)
+
+
+@pytest.mark.parametrize("T,d,gate,form", [(2000, 264, "rows", "int8"), (900, 5120, "shared", "e4m3"), (1000, 4096, "shared", "int8"), (700, 1024, "none", "bf16"),
+                                           (400, 6152, "rows", "e4m3"), (500, 8192, "shared", "bf16"), (400, 16384, "rows", "bf16"), (310, 16384, "none", "int8")])
+def test_backward_of_many_rows(T, d, gate, form):
+    test_backward(T, d, gate, True, form)
+
+
 def test_backward_parts_that_are_not_there():
     """Only dx, only dh_new, frozen norms: what is left out changes nothing else; the same bits with and without the sums."""
     import torch

@@ -1,8 +1,10 @@
 """Adapter gradients with x as bf16 rows or an 8-bit checkpoint, against a float64 statement on the values that the rows stand for.
 
-Tolerance.  u and v enter the second product as two bf16 values, off by 2^-17 of themselves at most; sums of K and of T terms run in fp32, on the
-tensor cores in steps of 16 that may each cut off a bit: K/16 + T/16 + 32 steps of 2^-23.  Both of the sum of the absolute values of the
-terms.  The Frobenius error, where such errors average out, is held to 2e-5."""
+Tolerance.  u and v are fp32 and enter the second product as three bf16 values, which is all of them.  Sums of K and of T terms run in fp32: on the
+tensor cores in steps of 16 that may each cut off a bit, at most 32 of them before the sum is taken out, and then in one rounded addition for
+512 terms.  So min(K / 16, 32) + K / 512 steps of 2^-23, the same of T, and 32 for scale, split and the joining of parts, of the sum of the absolute
+values of the terms.  The Frobenius error: 32 additions that lose half a unit of 2^-23 each, always towards zero, of partial sums that are half of the
+whole on average, in either product: 2 * 32 * 2^-25 = 1.9e-6; held to 3e-6."""
 import numpy as np
 import pytest
 
@@ -69,7 +71,8 @@ class Case:
         ents = [(r, s, plain.widen(A), plain.widen(B)) for r, s, A, B in zip(self.ranks, self.scales, self.A, self.B)]
         refs = plain.gradients(plain.kept(self.x, form), plain.widen(self.dy), ents, self.offsets, self.seg_entry)
         add = base if not written else 0.0
-        c = 2.0 ** -17 + (max(self.K, self.N) / 16 + self.T / 16 + 32) * 2.0 ** -23
+        steps = lambda n: min(n / 16, 32) + n / 512  # noqa: E731
+        c = (steps(max(self.K, self.N)) + steps(self.T) + 32) * 2.0 ** -23
         for e, (rA, rB, mA, mB) in enumerate(refs):
             s, r = self.slots[e], self.ranks[e]
             gA, gB = dA[s, :r] - add, dB[s, :, :r] - add
@@ -77,7 +80,7 @@ class Case:
                 bad = np.abs(got - ref) - (c * size + 2.0 ** -23 * abs(add))
                 assert (bad <= 0).all(), (e, float(bad.max()))
                 if np.linalg.norm(ref) > 0 and not add:
-                    assert np.linalg.norm(got - ref) <= 2e-5 * np.linalg.norm(ref), (e, np.linalg.norm(got - ref) / np.linalg.norm(ref))
+                    assert np.linalg.norm(got - ref) <= 3e-6 * np.linalg.norm(ref), (e, np.linalg.norm(got - ref) / np.linalg.norm(ref))
             dA[s, :r], dB[s, :, :r] = base, base
         assert (dA == base).all() and (dB == base).all(), "rows behind the rank, or free slots, were written"
 
@@ -99,6 +102,11 @@ CASES = [
     (700, 1024, 512, [32], [700], [0]),
     (1100, 520, 264, [16, 48], [127, 129, 500, 344], [0, 1, 0, 1]),
     (2100, 256, 384, [16], [2000, 100], [0, -1]),
+    (40, 5128, 8, [16], [40], [0]),                                    # sums that are taken out of the accumulators, steps of one half
+    (3000, 264, 8, [64, 8], [2900, 100], [0, 1]),
+    (257, 8, 328, [33], [257], [0]),
+    (449, 712, 72, [16, 64], [192, 64, 65, 128], [0, 1, 0, 1]),
+    (30, 544, 2056, [8, 16, 32, 64, 8, 16, 32], [1, 2, 1, 1, 0, 3, 1, 1, 1, 2, 1, 1, 2, 0, 1, 3, 1, 1, 1, 2, 1, 1, 1, 1], [k % 7 for k in range(24)]),
 ]
 
 
