@@ -718,47 +718,43 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_shrink_kernel(const __grid
 
 // ---- second pass -----------------------------------------------------------------------------------------
 // Items: slots in use in order, of each the column tiles (x first, then dy), of each its units.  A CTA has its part of the line, or, if
-// there are few items, whole ones.
+// there are few items, whole ones.  In the line an item is as long as it has units, but at least as long as finishing it takes in steps; what is
+// behind its units is nobody's work.  (Counted by units alone, the CTAs with the items of an adapter of few tokens and 64 ranks were still at it when
+// all others had left: 192 us for 8192 tokens, 114 of them of such a one,
+// that take 134 so.)
+constexpr int kRgFinishSteps = 2;
+__device__ __forceinline__ int item_length(int units, int r16) { return max(units, kRgFinishSteps + r16 / 16); }
 struct GradTasks {
     const RowsGradParams& p;
     const RgCtrl* c;
     unsigned long long mask;   // slots from here on
     int w, end, base = 0;   // base: of the slot at hand
-    int slot = 0, units = 0, tile = 0, a = 0, b = 0;
+    int slot = 0, units = 0, length = 0, tile = 0, a = 0, b = 0;
     __device__ GradTasks(const RowsGradParams& p_, const RgCtrl* c_, int w0, int w1) : p(p_), c(c_), mask(c_->used()), w(w0), end(w1) {}
     __device__ void next_slot()
     {
-        base += units * p.all_tiles;
+        base += length * p.all_tiles;
         slot = __ffsll((long long)mask) - 1;
         mask &= mask - 1ull;
         units = c->units[slot];
+        length = p.whole_items ? 1 : item_length(units, chunks_of_rank(p.snap[0].rank[slot]) * kChunk);
     }
     __device__ bool next()
     {
-        if (p.whole_items) {   // w, end, base: items here
-            if (b > 0) w += gridDim.x;
+        if (b > 0) w = p.whole_items ? w + gridDim.x : base + tile * length + (b < units ? b : length);
+        for (;; w = base + (tile + 1) * length) {
             if (w >= end) return false;
-            while (units == 0 || w >= base + p.all_tiles) {
-                if (units) base += p.all_tiles;
-                slot = __ffsll((long long)mask) - 1;
-                mask &= mask - 1ull;
-                units = c->units[slot];
-            }
-            tile = (int)(w - base);
-            a = 0; b = units;
-            return true;
+            while (w >= base + length * p.all_tiles) next_slot();
+            tile = (w - base) / length;
+            a = w - base - tile * length;
+            if (a < units) break;
         }
-        w += b - a;
-        if (w >= end) return false;
-        while (w >= base + units * p.all_tiles) next_slot();
-        const int in = w - base;
-        tile = in / units;
-        a = in - tile * units;
-        b = min(units, a + (end - w));
+        b = p.whole_items ? units : min(units, a + (end - w));
         return true;
     }
     __device__ bool whole() const { return b - a == units; }
-    __device__ bool last() const { return p.whole_items ? w + gridDim.x >= end : w + (b - a) >= end; }   // of this CTA's
+    // of this CTA's: what follows is not there, or not its own, or behind an item's units
+    __device__ bool last() const { return (p.whole_items ? w + (int)gridDim.x : b < units ? w + (b - a) : base + (tile + 1) * length) >= end; }
     __device__ int item() const { return w - a; }
     __device__ int job() const { return tile < p.tiles[0] ? 0 : 1; }
     __device__ int column() const { return (tile < p.tiles[0] ? tile : tile - p.tiles[0]) * 128; }
@@ -848,7 +844,10 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_grad_kernel(const __grid_c
     }
     __syncthreads();
     int total = 0;
-    for (unsigned long long m = c->used(); m; m &= m - 1ull) total += p.whole_items ? 1 : c->units[__ffsll((long long)m) - 1];
+    for (unsigned long long m = c->used(); m; m &= m - 1ull) {
+        const int s = __ffsll((long long)m) - 1;
+        total += p.whole_items ? 1 : item_length(c->units[s], chunks_of_rank(p.snap[0].rank[s]) * kChunk);
+    }
     const RgLine line(total * p.all_tiles);
     const int w0 = p.whole_items ? (int)blockIdx.x : line.begin((int)blockIdx.x), w1 = p.whole_items ? line.W : line.begin((int)blockIdx.x + 1);
 
@@ -872,7 +871,7 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_grad_kernel(const __grid_c
         }
         return u.turn;
     };
-    if (w0 < w1) {
+    if (GradTasks(p, c, w0, w1).next()) {   // (a part can lie behind the units of an item)
         if (warp == 0) {
             if (elect_one()) {
                 const CUtensorMap* map = nullptr;
