@@ -558,7 +558,7 @@ __global__ void __launch_bounds__(32 * kSumSlices) norm_sums_kernel(const __grid
 cudaError_t launch_block_norm(const NormForward& a, int num_sms, cudaStream_t stream)
 {
     // As few vectors per thread as the warps allow where there are rows for one wave at most: what counts is one row's time.  Two for more, to
-    // some 40 rows per SM (2000 x 4096 with all that there is: 12.3 us, four 14.7; 3000 x 4096 16.6 for 2900 and 19.5), four beyond, where
+    // some 40 rows per SM (2000 x 4096 with all that there is: 12.3 us, four 14.7; 3000 x 4096 17.3 and 19.5), four beyond, where
     // what counts is loads in flight (8192 x 4096 without o: 22.4 us, 6.0 TB/s, two 24.7; 16384 x 2048 21.7 and 27.1).  The weights are asked
     // for ahead of the sums up to a few waves (40 x 4096 with a gate per token: 2.5 us, 3.4 behind them); beyond they come from L1, and the
     // registers are better used for more rows (8192 x 4096: 26.4 us with two vectors, 29.8 ahead).  T and d decide and nothing else: a call on h'

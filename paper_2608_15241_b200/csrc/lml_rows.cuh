@@ -141,22 +141,30 @@ __device__ __forceinline__ uint32_t amax_bits(const uint4& v)   // largest |valu
     return max(a & 0xffffu, a >> 16);
 }
 
-// Vector `vec` (columns 8 vec ...) of row t of a checkpoint, by the 32 lanes of a converged warp that hold consecutive
-// vectors, the first a multiple of 32.  Lanes behind the last column pass zeros.
-__device__ __forceinline__ void store_kept(const Rows& r, int T, int d, long long t, int vec, const uint4& v)
+// Vector `vec` (columns 8 vec ...) of a row of a checkpoint, by the 32 lanes of a converged warp that hold consecutive vectors, the first a multiple
+// of 32.  to: where the vector's bytes go; word_to: the row's scale word of these columns (what of them is behind the row is not written).  Lanes
+// behind the last column pass zeros.
+template <bool E4M3>
+__device__ __forceinline__ void store_vector(uint8_t* to, uint32_t* word_to, bool there, int vec, const uint4& v)
 {
     uint32_t amax = amax_bits(v);
     amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
     amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-    const bool e4m3 = r.format == kE4m3;
-    const int pitch = kept_pitch(d);
-    const uint32_t byte = byte_of_amax(amax, e4m3);
-    if (vec * 8 < pitch) *reinterpret_cast<uint2*>(static_cast<uint8_t*>(r.data) + t * pitch + vec * 8) =
-            encode8(v, byte, e4m3);
-    uint32_t word = vec * 8 < pitch ? byte << (8 * ((vec >> 2) & 3)) : 0u;   // (blocks behind the last have scale byte 0)
+    const uint32_t byte = byte_of_amax(amax, E4M3);
+    if (there) *reinterpret_cast<uint2*>(to) = encode8(v, byte, E4M3);
+    uint32_t word = there ? byte << (8 * ((vec >> 2) & 3)) : 0u;   // (blocks behind the last have scale byte 0)
     word |= __shfl_xor_sync(0xffffffffu, word, 4);
     word |= __shfl_xor_sync(0xffffffffu, word, 8);
-    if ((vec & 15) == 0 && vec * 8 < pitch) r.scales[(long long)(vec >> 4) * T + t] = word;
+    if ((vec & 15) == 0 && there) *word_to = word;
+}
+__device__ __forceinline__ void store_kept(const Rows& r, int T, int d, long long t, int vec, const uint4& v)
+{
+    const int pitch = kept_pitch(d);
+    const bool there = vec * 8 < pitch;
+    uint8_t* to = static_cast<uint8_t*>(r.data) + t * pitch + vec * 8;
+    uint32_t* word_to = r.scales + (long long)(vec >> 4) * T + t;
+    if (r.format == kE4m3) store_vector<true>(to, word_to, there, vec, v);
+    else store_vector<false>(to, word_to, there, vec, v);
 }
 // Ordinary loads, not through the non-coherent path: the kernels start while the work that writes their inputs still runs, and
 // an output may be the buffer of an input.
@@ -178,16 +186,6 @@ __device__ __forceinline__ uint4 ld_weights(const void* p, int vec)   // (kept i
     asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(static_cast<const uint4*>(p) + vec) : "memory");
     return v;
 }
-// The vector as packed bf16; vec within the row.
-__device__ __forceinline__ uint4 load_rows(const Rows& r, int T, int d, long long t, int vec)
-{
-    if (r.format == kBf16) return ld_v4(static_cast<const __nv_bfloat16*>(r.data) + t * d + vec * 8);
-    const uint2 q = ld_v2(static_cast<const uint8_t*>(r.data) + t * kept_pitch(d) + vec * 8);
-    const uint32_t word = ld_after_wait(r.scales + (long long)(vec >> 4) * T + t);
-    const uint32_t byte = (word >> (8 * ((vec >> 2) & 3))) & 0xffu;
-    return r.format == kE4m3 ? decode8<true>(q, byte) : decode8<false>(q, byte);
-}
-
 // ---- launchers ------------------------------------------------------------------------------------
 cudaError_t launch_kept_store(const void* x, int T, int d, const Rows& out, cudaStream_t stream);
 cudaError_t launch_kept_load(const Rows& in, int T, int d, void* x, cudaStream_t stream);

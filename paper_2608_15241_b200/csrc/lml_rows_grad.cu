@@ -25,7 +25,10 @@
 // dA and dB are fp32 and so are u and v on the way: each goes into the second product as three bf16 values whose sum is the fp32
 // value, side by side as 3r columns of one product.  One bf16 value would leave 2^-9, 1e-3 of every gradient, two 3e-6.
 //
-// Bound by memory: x and dy leave HBM once (the second pass finds them in L2 up to about 100 MB).
+// x and dy leave HBM once (the second pass finds them in L2 up to about 100 MB), but memory is not what bounds it: 8192 x 11008 in E4M3 and 4096,
+// eight adapters of 8 to 64 ranks, take 142 us where the bytes take 28.  It is the way of a stage through its ring, load, conversion, product and
+// back, some 4000 cycles; no role is busy for more than half of the time, and without the conversion it is 11 % less, without the other
+// operand 1 %, without the tiles' loads 8 %.  Small calls (100 tokens of one adapter 17 us) are made of a dozen such latencies in a row.
 #include <cstring>
 
 #include "lml_ptx_sm100.cuh"
