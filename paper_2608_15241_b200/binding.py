@@ -420,7 +420,7 @@ def _stream(stream) -> int:
 
 
 _raw_stream_of = None
-_bf16 = None
+_bf16 = _f32 = _u8 = None
 
 
 def _stream_on(device: int, stream) -> int:
@@ -448,13 +448,24 @@ def _bf16_rows(t, shape, name, device: int) -> int:
     return t.data_ptr()
 
 
-def _sums(t, d, name, device: int) -> int:
+def _sums(t, shape, name, device: int) -> int:
     """Checks a float32 [d] tensor that a call adds to, and gives its address; None is 0."""
     if t is None:
         return 0
-    import torch
-    assert t.dtype is torch.float32 and t.shape == (d,) and t.is_contiguous() and t.get_device() == device, (name, t.shape, t.dtype)
+    global _f32
+    if _f32 is None:
+        import torch
+        _f32 = torch.float32
+    assert t.dtype is _f32 and t.shape == shape and t.is_contiguous() and t.get_device() == device, (name, t.shape, t.dtype)
     return t.data_ptr()
+
+
+def _kept_uint8(t, shape, name, device: int) -> None:
+    global _u8
+    if _u8 is None:
+        import torch
+        _u8 = torch.uint8
+    assert t.dtype is _u8 and t.shape == shape and t.is_contiguous() and t.get_device() == device, (name, t.shape, t.dtype)
 
 
 def _cuda_index(t, name) -> int:
@@ -467,24 +478,52 @@ class Checkpoint:
     data uint8 [T][width up to a multiple of 32], scales uint8 [ceil(width / 128)][T][4]."""
 
     def __init__(self, data, scales, width: int, form: str):
-        import torch
-        T = int(data.shape[0])
+        T = data.shape[0]
         assert form in ("int8", "e4m3"), form
         self.device = _cuda_index(data, "data")
-        assert data.dtype is torch.uint8 and scales.dtype is torch.uint8 and scales.get_device() == self.device
-        assert data.is_contiguous() and scales.is_contiguous() and width > 0 and width % 8 == 0
-        assert data.shape == (T, (width + 31) // 32 * 32) and scales.shape == ((width + 127) // 128, T, 4), (data.shape, scales.shape)
-        self.data, self.scales, self.tokens, self.width, self.form = data, scales, T, int(width), form
+        _kept_uint8(data, (T, (width + 31) // 32 * 32), "data", self.device)
+        _kept_uint8(scales, ((width + 127) // 128, T, 4), "scales", self.device)
+        assert width > 0 and width % 8 == 0, width
+        self._data, self._scales, self.tokens, self.width, self.form = data, scales, T, int(width), form
         self.rows = Rows(data.data_ptr(), scales.data_ptr(), ROW_FORMS[form])
 
     @classmethod
     def empty(cls, tokens: int, width: int, form: str, device="cuda") -> "Checkpoint":
         import torch
-        return cls(torch.empty((tokens, (width + 31) // 32 * 32), dtype=torch.uint8, device=device),
-                   torch.empty(((width + 127) // 128, tokens, 4), dtype=torch.uint8, device=device), width, form)
+        return cls._in(torch.empty(cls._bytes(tokens, width), dtype=torch.uint8, device=device), tokens, width, form)
+
+    @staticmethod
+    def _bytes(tokens: int, width: int) -> int:
+        return tokens * ((width + 31) // 32 * 32 + (width + 127) // 128 * 4)
+
+    @classmethod
+    def _in(cls, buffer, tokens: int, width: int, form: str) -> "Checkpoint":
+        """Both arrays in one buffer (one allocation instead of two views of it: they are made when somebody asks for them)."""
+        assert form in ("int8", "e4m3") and width > 0 and width % 8 == 0, (form, width)
+        self = cls.__new__(cls)
+        self.device = _cuda_index(buffer, "device")
+        self.tokens, self.width, self.form = tokens, width, form
+        self._data = self._scales = None
+        self._buffer, at = buffer, buffer.data_ptr()
+        self.rows = Rows(at, at + tokens * ((width + 31) // 32 * 32), ROW_FORMS[form])
+        return self
+
+    @property
+    def data(self):
+        if self._data is None:
+            pitch = (self.width + 31) // 32 * 32
+            self._data = self._buffer[:self.tokens * pitch].view(self.tokens, pitch)
+        return self._data
+
+    @property
+    def scales(self):
+        if self._scales is None:
+            groups = (self.width + 127) // 128
+            self._scales = self._buffer[self.tokens * ((self.width + 31) // 32 * 32):].view(groups, self.tokens, 4)
+        return self._scales
 
     def nbytes(self) -> int:
-        return int(self.data.numel() + self.scales.numel())
+        return self._bytes(self.tokens, self.width)
 
     def store(self, x, stream=None) -> "Checkpoint":
         """Keep x (bf16 [tokens][width])."""
@@ -497,14 +536,19 @@ class Checkpoint:
         import torch
         shape, dev = (self.tokens, self.width), self.device
         if out is None:
-            out = torch.empty(shape, dtype=torch.bfloat16, device=self.data.device)
-        lml_checkpoint_load(dev, self.rows, self.tokens, self.width, _bf16_rows(out, shape, "out", dev), _stream_on(dev, stream))
+            out = (self._data if self._data is not None else self._buffer).new_empty(shape, dtype=torch.bfloat16)
+            at = out.data_ptr()
+        else:
+            at = _bf16_rows(out, shape, "out", dev)
+        lml_checkpoint_load(dev, self.rows, self.tokens, self.width, at, _stream_on(dev, stream))
         return out
 
 
 def checkpoint_store(x, form: str = "int8", stream=None) -> Checkpoint:
     """A new checkpoint of x (bf16 [T][d])."""
-    return Checkpoint.empty(int(x.shape[0]), int(x.shape[1]), form, x.device).store(x, stream)
+    import torch
+    T, d = x.shape
+    return Checkpoint._in(x.new_empty(Checkpoint._bytes(T, d), dtype=torch.uint8), T, d, form).store(x, stream)
 
 
 def _as_rows(x, shape, name, device: int):
@@ -542,11 +586,16 @@ class BlockNorm:
         h_at = _bf16_rows(h, shape, "h", dev)
         if h_new is None and o is not None:
             h_new = torch.empty_like(h)
+            h_new_at = h_new.data_ptr()
+        else:
+            h_new_at = _bf16_rows(h_new, shape, "h_new", dev)
         if x is None and self.w_pre is not None:
             x = torch.empty_like(h)
-        lml_block_norm(dev, self.desc, T, h_at, _bf16_rows(o, shape, "o", dev), _bf16_rows(gate_rows, shape, "gate_rows", dev),
-                       _bf16_rows(h_new, shape, "h_new", dev), _bf16_rows(x, shape, "x", dev), _as_rows(x_checkpoint, shape, "x_checkpoint", dev),
-                       _as_rows(h_checkpoint, shape, "h_checkpoint", dev), _stream_on(dev, stream))
+            x_at = x.data_ptr()
+        else:
+            x_at = _bf16_rows(x, shape, "x", dev)
+        lml_block_norm(dev, self.desc, T, h_at, _bf16_rows(o, shape, "o", dev), _bf16_rows(gate_rows, shape, "gate_rows", dev), h_new_at, x_at,
+                       _as_rows(x_checkpoint, shape, "x_checkpoint", dev), _as_rows(h_checkpoint, shape, "h_checkpoint", dev), _stream_on(dev, stream))
         return (h if o is None else h_new), x
 
     def backward(self, h_new, o, dx, dh_new, gate_rows=None, dh=None, d_o=None, dw_pre=None, dw_post=None, dgate=None, workspace=None,
@@ -563,19 +612,26 @@ class BlockNorm:
         gate_at = _bf16_rows(gate_rows, shape, "gate_rows", dev)
         if dh is None:
             dh = torch.empty_like(some)
+            dh_at = dh.data_ptr()
+        else:
+            dh_at = _bf16_rows(dh, shape, "dh", dev)
         if d_o is None and o is not None:
             d_o = torch.empty_like(some)
+            d_o_at = d_o.data_ptr()
+        else:
+            d_o_at = _bf16_rows(d_o, shape, "d_o", dev)
         dgate_rows = torch.empty_like(gate_rows) if gate_rows is not None else None
         n_ws = 0
         if dw_pre is not None or dw_post is not None or dgate is not None:
             if workspace is None:
-                workspace = torch.empty(max(lml_block_norm_workspace_bytes(dev, T, d), 256), dtype=torch.uint8, device=some.device)
-            assert workspace.get_device() == dev, "workspace"
-            n_ws = workspace.numel()
+                n_ws = max(lml_block_norm_workspace_bytes(dev, T, d), 256)
+                workspace = some.new_empty(n_ws, dtype=torch.uint8)
+            else:
+                assert workspace.get_device() == dev and workspace.is_contiguous(), "workspace"
+                n_ws = workspace.numel() * workspace.element_size()
         lml_block_norm_backward(dev, self.desc, T, _as_rows(h_new, shape, "h_new", dev), _as_rows(o, shape, "o", dev), gate_at, dx_at, dh_new_at,
-                                _bf16_rows(dh, shape, "dh", dev), _bf16_rows(d_o, shape, "d_o", dev), _sums(dw_pre, d, "dw_pre", dev),
-                                _sums(dw_post, d, "dw_post", dev), _sums(dgate, d, "dgate", dev), _ptr(dgate_rows),
-                                _ptr(workspace) if n_ws else 0, n_ws, _stream_on(dev, stream))
+                                dh_at, d_o_at, _sums(dw_pre, (d,), "dw_pre", dev), _sums(dw_post, (d,), "dw_post", dev),
+                                _sums(dgate, (d,), "dgate", dev), _ptr(dgate_rows), _ptr(workspace) if n_ws else 0, n_ws, _stream_on(dev, stream))
         return dh, d_o, (dgate_rows if gate_rows is not None else dgate)
 
 
@@ -753,11 +809,12 @@ class Table:
             assert t.get_device() == dev, t.device
         dy_at = _bf16_rows(dy, (T, self.d_out), "dy", dev)
         if workspace is None:
-            workspace = torch.empty(max(lml_backward_rows_workspace_bytes(self.handle, T, G), 256), dtype=torch.uint8, device=dy.device)
-        assert workspace.get_device() == dev, "workspace"
+            workspace = dy.new_empty(max(lml_backward_rows_workspace_bytes(self.handle, T, G), 256), dtype=torch.uint8)
+        assert workspace.get_device() == dev and workspace.is_contiguous(), "workspace"
         lora_mixed_linear_backward_adapters_rows(self.handle, table_T.handle, _as_rows(x, (T, self.d_in), "x", dev), dy_at, T,
                                                  seg_offsets.data_ptr(), slot_ids.data_ptr(), slot_ids_T.data_ptr(), G, dA.data_ptr(),
-                                                 dB.data_ptr(), accumulate, workspace.data_ptr(), workspace.numel(), _stream_on(dev, stream))
+                                                 dB.data_ptr(), accumulate, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                                 _stream_on(dev, stream))
 
     def lora_mixed_linear_dual(self, x, W0, seg_offsets, slot_ids_a, slot_ids_b, perm=None, stream=None):
         """-> (y_a, y_b): the layer under two slot bindings of the same segments."""

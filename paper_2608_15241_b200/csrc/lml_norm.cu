@@ -354,11 +354,10 @@ __global__ void __launch_bounds__(32 * norm_warps(V), 1) block_norm_backward_ker
     const size_t where_step = (size_t)step * d;
     int stage = 0, turn = 0;
     uint32_t phase = 0;
-    // (After a wait that gave up the row's results are whatever the stage holds; there is nobody to tell but the next check of the device.)
     for (unsigned t = first; t < (unsigned)T; t += step, turn ^= 1, where0 += where_step) {
         const uint8_t* at = ring + (size_t)stage * L.stage_bytes;
         const uint32_t* wh = reinterpret_cast<const uint32_t*>(at + L.at_words);
-        if (!mbar_try_wait(smem_u32(&bars[stage]), phase)) mbar_wait(smem_u32(&bars[stage]), phase, &gave_up);
+        const bool arrived = mbar_try_wait(smem_u32(&bars[stage]), phase) || mbar_wait(smem_u32(&bars[stage]), phase, &gave_up);
         __syncwarp();
         // h'^2, o^2, dx w_pre h' (mean(dx w_pre hh) = rho mean(dx w_pre h')), and dh', dx w_pre and h' by z
         Eight<kPacked> hp[V], op[V];
@@ -382,6 +381,7 @@ __global__ void __launch_bounds__(32 * norm_warps(V), 1) block_norm_backward_ker
             else op[i].set(zero);
             if (has_dh_new && ok) ld_stage(qp[i], at + L.at_dh, vec, kBf16, nullptr);
             else qp[i].set(zero);
+            if (!arrived) qp[i].set(make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u));   // (a wait gave up: its results are NaN)
             float2 h[4], g[4], o[4], q[4], w[4], gate[4];
             hp[i].get(h); gp[i].get(g); op[i].get(o); qp[i].get(q); w_pre[i].get(w);
             if (row_gate) unpack_pairs(ok ? *reinterpret_cast<const uint4*>(at + L.at_gate + vec * 16) : zero, gate);

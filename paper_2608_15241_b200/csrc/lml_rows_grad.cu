@@ -76,8 +76,8 @@ struct alignas(64) RowsGradParams {
 };
 
 // What the producer says about a stage.
-// first, last of an item; last of this CTA; goes through the converting warps; the right half of 128 columns
-constexpr int kRgFirst = 1, kRgLast = 2, kRgEnd = 4, kRgTouched = 8, kRgRight = 16;
+// last of an item; last of this CTA; goes through the converting warps; the right half of 128 columns
+constexpr int kRgLast = 1, kRgEnd = 2, kRgTouched = 4, kRgRight = 8;
 struct RgInfo {
     int flags, valid;   // rows
     int r16;            // columns of the other operand (second pass: of each of its three parts)
@@ -583,18 +583,17 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_shrink_kernel(const __grid
         if (warp == 0) {
             if (elect_one()) {
                 const CUtensorMap* map = nullptr;
-                bool raw = false, first = false;
+                bool raw = false;
                 int r16 = 0, valid = 0, row = 0;
                 uint32_t words_at = 0;   // in words of four bytes; what counts is where they lie to 16
                 each([&](const ShrinkTasks& t) {
                          map = &p.map[0][t.job]; row = t.row; valid = t.valid;
                          r16 = chunks_of_rank(p.snap[t.job].rank[t.slot]) * kChunk;
-                         raw = FMT != kBf16 && t.job == 0; first = true;
+                         raw = FMT != kBf16 && t.job == 0;
                          words_at = (uint32_t)(reinterpret_cast<uintptr_t>(p.scales) >> 2) + (uint32_t)t.row;
                      },
                      [&](RgCursor& u, int k, int half, int last) {
-                         const int flags = last | (raw ? kRgTouched : 0) | (first ? kRgFirst : 0) | (half ? kRgRight : 0);
-                         first = false;
+                         const int flags = last | (raw ? kRgTouched : 0) | (half ? kRgRight : 0);
                          c->info[u.stage] = {flags, valid, r16, raw ? (int)((words_at + (uint32_t)(k >> 7) * (uint32_t)p.T) & 3u) : -1};
                          load_tile<false>(c, map, u.at, u.stage, raw, row, k + 64 * half);
                      });
@@ -859,15 +858,13 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_grad_kernel(const __grid_c
         RgCursor u(ring);
         for (GradTasks t(p, c, w0, w1); t.next();) {
             const bool raw = FMT != kBf16 && t.job() == 0, end = t.last();
-            int first = kRgFirst;
             item(t, raw);
             for (RgPieces v(c, t); v.next();) {
                 const int valid = v.valid(), n = halves(0, valid);
                 for (int half = 0; half < n; ++half, u.advance()) {
                     if (!mbar_wait(smem_u32(&c->empty[u.stage]), u.phase ^ 1u, abort)) return u.turn;
                     const int rows = min(valid - 64 * half, 64);
-                    const int flags = first | (raw || (rows & 15) ? kRgTouched : 0) | (v.left == 0 && half + 1 == n ? end ? kRgLast | kRgEnd : kRgLast : 0);
-                    first = 0;
+                    const int flags = (raw || (rows & 15) ? kRgTouched : 0) | (v.left == 0 && half + 1 == n ? end ? kRgLast | kRgEnd : kRgLast : 0);
                     f(u, v, half, rows, flags);
                 }
             }
