@@ -262,18 +262,14 @@ __device__ __forceinline__ void post_turn(RgCtrl* c, int turn, int stage, uint32
     mbar_arrive(smem_u32(&c->turn[turn % kRgTurns]));   // (releases what was written)
 }
 // ... the words of half a step's rows into the stage, from `words` on.  A bulk copy wants 16-byte boundaries, so it begins up to three words
-// early, and takes so many more; where that would reach behind the array's end (`last`), ordinary loads bring the rest.
+// early, and takes so many more.  That reaches into the rows behind and the next groups of columns, and with few rows behind the array's
+// end (10 rows: 13 groups on): then ordinary loads bring what does not fill 16 bytes.
 template <bool SECOND>
-__device__ __forceinline__ void load_words(RgCtrl* c, int stage, const uint32_t* words, bool last, const uint32_t* words_end)
+__device__ __forceinline__ void load_words(RgCtrl* c, int stage, const uint32_t* words, const uint32_t* words_end)
 {
     constexpr int kWords = SECOND ? 72 : kRgWords;
     const uint32_t bar = smem_u32(&c->full[stage]);
     const uint32_t* from = reinterpret_cast<const uint32_t*>(reinterpret_cast<uintptr_t>(words) & ~(uintptr_t)15);
-    if (!last) {
-        mbar_arrive_expect_tx(bar, kWords * 4);
-        bulk_load(smem_u32(c->words[stage]), from, kWords * 4, bar);
-        return;
-    }
     uint32_t bytes = kWords * 4;
     if (words_end - from < kWords) {
         bytes = (uint32_t)(words_end - from) * 4u & ~15u;
@@ -617,17 +613,15 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_shrink_kernel(const __grid
             if (elect_one()) {
                 const uint32_t *words = nullptr, *words_end = p.scales + (size_t)kept_groups(p.d[0]) * p.T;
                 bool raw = false;
-                bool last = false;
                 const int turns = each([&](const ShrinkTasks& t) {
                         raw = FMT != kBf16 && t.job == 0;
                         words = p.scales + t.row + (size_t)t.step * p.T;
-                        last = t.step + t.n == p.tiles[0];
                     },
                     [&](RgCursor& u, int, int half, int) {
                         if (!raw) {
                             mbar_arrive(smem_u32(&c->full[u.stage]));
                         } else {
-                            load_words<false>(c, u.stage, words, last, words_end);
+                            load_words<false>(c, u.stage, words, words_end);
                             if (half) words += p.T;   // (a step with one half is the last)
                             post_turn(c, u.turn, u.stage, u.phase);
                             ++u.turn;
@@ -907,10 +901,10 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_grad_kernel(const __grid_c
         } else if (warp == kRgWordsWarp) {
             if (elect_one()) {
                 const uint32_t *words = nullptr, *words_end = p.scales + (size_t)kept_groups(p.d[0]) * p.T;
-                bool is_raw = false, last = false;
-                const int turns = each([&](const GradTasks& t, bool raw) { is_raw = raw; words = p.scales + (size_t)t.tile * p.T; last = t.tile + 1 == p.tiles[0]; },
+                bool is_raw = false;
+                const int turns = each([&](const GradTasks& t, bool raw) { is_raw = raw; words = p.scales + (size_t)t.tile * p.T; },
                     [&](RgCursor& u, const RgPieces& v, int half, int, int flags) {
-                        if (is_raw) load_words<true>(c, u.stage, words + v.row() + 64 * half, last, words_end);
+                        if (is_raw) load_words<true>(c, u.stage, words + v.row() + 64 * half, words_end);
                         else mbar_arrive(smem_u32(&c->full[u.stage]));
                         if (flags & kRgTouched) { post_turn(c, u.turn, u.stage, u.phase); ++u.turn; }
                     });

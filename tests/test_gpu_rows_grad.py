@@ -118,6 +118,27 @@ def test_gradients(T, K, N, ranks, lengths, seg_entry, form):
     c.close()
 
 
+@pytest.mark.parametrize("T,lengths", [(1, [1, 0]), (10, [7, 3]), (70, [66, 4]), (137, [3, 134])])
+@pytest.mark.parametrize("K", (368, 4096))
+def test_scale_words_that_end_where_the_memory_ends(T, lengths, K):
+    """The words of a tile's rows come in whole pieces of 16 bytes, more than there are rows; nothing behind the array may be read."""
+    import torch
+    from paper_2608_15241_b200 import binding as b
+    c = Case(T, K, 264, [16, 33], lengths, [0, 1])
+    want = c.run("int8")
+    kept = c.rows("int8")
+    buffer = torch.empty(22 << 20, dtype=torch.uint8, device="cuda")          # a block of memory of its own, without a rest
+    n, m = kept.scales.numel(), kept.data.numel()
+    at = (buffer.numel() - n) // 16 * 16                                      # (both arrays are 16-byte aligned)
+    scales, data = buffer[at:at + n].view(kept.scales.shape), buffer[:m].view(kept.data.shape)
+    scales.copy_(kept.scales)
+    data.copy_(kept.data)
+    got = c.run("int8", x=b.Checkpoint(data, scales, K, "int8"))
+    assert np.array_equal(got[0], want[0]) and np.array_equal(got[1], want[1])
+    c.check(*got, "int8")
+    c.close()
+
+
 @pytest.mark.parametrize("form", ("int8", "bf16"))
 def test_accumulated_over_batches_and_the_same_bits_again(form):
     c = Case(300, 264, 136, [4, 16, 33], [40, 0, 100, 3, 57, 100], [0, 1, 2, 1, -1, 0])
