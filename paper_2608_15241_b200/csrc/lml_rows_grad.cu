@@ -28,7 +28,7 @@
 // x and dy leave HBM once (the second pass finds them in L2 up to about 100 MB), but memory is not what bounds it: 8192 x 11008 in E4M3 and 4096,
 // eight adapters of 8 to 64 ranks, take 142 us where the bytes take 28.  It is the way of a stage through its ring, load, conversion, product and
 // back, some 4000 cycles; no role is busy for more than half of the time, and without the conversion it is 11 % less, without the other
-// operand 1 %, without the tiles' loads 8 %.  Small calls (100 tokens of one adapter 17 us) are made of a dozen such latencies in a row.
+// operand 1 %, without the tiles' loads 8 %.  Small calls (100 tokens of one adapter 16 us) are made of a dozen such latencies in a row.
 #include <cstring>
 
 #include "lml_ptx_sm100.cuh"
@@ -55,7 +55,7 @@ constexpr int kRgTurns = 16;                    // tiles on their way to and fro
 static_assert(kRgTurns >= kRgMaxStages + kRgGroups && (kRgTurns & (kRgTurns - 1)) == 0, "a turn's place must have been read before it is used again");
 constexpr int kRgWords = 136;                   // scale words of half a step, one per row, brought in from a 16-byte boundary on (of 64 rows: 72)
 constexpr int kRgChunk = 8;                     // half steps that one accumulator takes; see issue_steps
-constexpr int kRgLeast = 4;                     // steps of a CTA's part (of a whole pass, if it has fewer)
+constexpr int kRgLeast = 2;                     // steps of a CTA's part (of a whole pass, if it has fewer); 100 tokens of 4096 x 4096: 16.1 us, four 17.1
 
 struct alignas(64) RowsGradParams {
     CUtensorMap map[2][2];    // x, dy; first pass: boxes of 64 columns x 128 rows; second: 64 (8-bit x: 128) x 64
