@@ -7,15 +7,15 @@
 // rows_grad_kernel: dA and dB.  An item is (slot, 128 columns of x or dy), its work the slot's pieces.
 // A step of either is a tile of 128 rows x 128 columns, which goes through the rings in two halves along what is contracted: 64 columns in the
 // first pass, 64 rows in the second: a stage's way through loading, conversion and product is some 4000 cycles whatever its size, so
-// what counts is how many there are (beside 64 ranks eight and five, 145 us for 8192 x 11008 in E4M3 and 4096; with the 8 bits in a place of
-// their own six and four, 153).
+// what counts is how many there are (beside 64 ranks eight and five; with the 8 bits in a place of their own six and four, and 5 % more time
+// for 8192 x 11008 in E4M3 and 4096).
 // In both the work of all items stands in one line that is cut into equal parts, one per SM; a CTA walks its part without a pause
 // between items.  An item that the cuts divide is joined in device memory: every CTA writes its partial result, and the last one to
 // arrive adds them in the order of the parts, so the bits do not depend on who that is.  (A form with a cluster per item and an
 // exchange through distributed shared memory spent 10 us per CTA on setting up and joining.)
 //
-// Both are rings of tiles of x or dy as TMA brings them in, multiplied by tcgen05 into one of two accumulators.  Roles: three producers, of
-// tiles, of the other operand and of scale words (one thread for two of them is the slowest role: a copy costs it a few hundred cycles), the
+// Both are rings of tiles of x or dy as TMA brings them in, multiplied by tcgen05 into one of two accumulators.  Roles: two producers, of
+// tiles and of the other operand (one thread for both is the slowest role: a copy costs it a few hundred cycles), the
 // first of which tells the others what a stage holds; an issuer; four warps that finish items while the next one is multiplied;
 // groups of warps that take 8-bit tiles in turn through their registers and write them back in place as bf16 (exact: the
 // scales are powers of two) in the swizzled order of the tensor cores.  The second product contracts over tokens: the tile
@@ -26,7 +26,7 @@
 // value, side by side as 3r columns of one product.  One bf16 value would leave 2^-9, 1e-3 of every gradient, two 3e-6.
 //
 // x and dy leave HBM once (the second pass finds them in L2 up to about 100 MB), but memory is not what bounds it: 8192 x 11008 in E4M3 and 4096,
-// eight adapters of 8 to 64 ranks, take 142 us where the bytes take 28.  It is the way of a stage through its ring, load, conversion, product and
+// eight adapters of 8 to 64 ranks, take 144 us where the bytes take 28.  It is the way of a stage through its ring, load, conversion, product and
 // back, some 4000 cycles; no role is busy for more than half of the time, and without the conversion it is 11 % less, without the other
 // operand 1 %, without the tiles' loads 8 %.  Small calls (100 tokens of one adapter 16 us) are made of a dozen such latencies in a row.
 #include <cstring>
@@ -41,8 +41,7 @@ using namespace ptx;
 constexpr int kRgGroups = 2, kRgGroup = 8;      // converting groups, warps of each
 constexpr int kRgFinish = 4;                    // warps that finish items (warps 2 ... 5: one per quarter of the accumulator's lanes)
 constexpr int kRgOther = 2 + kRgFinish;         // the warp that brings in the other operand
-constexpr int kRgWordsWarp = kRgOther + 1;      // ... and the scale words
-constexpr int kRgFirstConv = kRgWordsWarp + 1;
+constexpr int kRgFirstConv = kRgOther + 1;
 constexpr int kRgThreads = 32 * (kRgFirstConv + kRgGroups * kRgGroup);
 constexpr int kRgSegs = 320;                    // segments of a launch; a call of more runs in slices
 constexpr int kRgTile = 128 * 64 * 2;           // bytes of half a step as it is multiplied: [row][64 columns], or two times [64 rows][64 columns]
@@ -50,10 +49,9 @@ constexpr int kRgHalfTile = kRgTile / 2;
 constexpr int kRgRaw = 128 * 64;                // ... of the 8 bits that it is made of, [128][64] or [64][128]
 constexpr int kRgPiece = 2 * 3 * kRankPad * 128;   // u (or v) of a piece: [64 tokens each][three parts][column][64]
 constexpr int kRgPartial = kRankPad * 128;      // floats of a partial result
-constexpr int kRgMaxStages = 10;
+constexpr int kRgMaxStages = 12;
 constexpr int kRgTurns = 16;                    // tiles on their way to and from the converting warps: as many as stages, and an end for each group
 static_assert(kRgTurns >= kRgMaxStages + kRgGroups && (kRgTurns & (kRgTurns - 1)) == 0, "a turn's place must have been read before it is used again");
-constexpr int kRgWords = 136;                   // scale words of half a step, one per row, brought in from a 16-byte boundary on (of 64 rows: 72)
 constexpr int kRgChunk = 8;                     // half steps that one accumulator takes; see issue_steps
 constexpr int kRgLeast = 2;                     // steps of a CTA's part (of a whole pass, if it has fewer); 100 tokens of 4096 x 4096: 16.1 us, four 17.1
 
@@ -76,14 +74,17 @@ struct alignas(64) RowsGradParams {
 };
 
 // What the producer says about a stage.
-// last of an item; last of this CTA; goes through the converting warps; the right half of 128 columns
-constexpr int kRgLast = 1, kRgEnd = 2, kRgTouched = 4, kRgRight = 8;
+constexpr int kRgLast = 1, kRgEnd = 2, kRgTouched = 4;   // last of an item; last of this CTA; goes through the converting warps
 struct RgInfo {
     int flags, valid;   // rows
     int r16;            // columns of the other operand (second pass: of each of its three parts)
-    int word;           // of a converted tile: place of its first scale word; -1: only rows behind the last are cleared
 };
-struct RgTurn { int stage, phase; };   // stage < 0: no more
+// ... to the converting warps, in 16 bytes.
+struct alignas(16) RgTurn {
+    int where;                // stage, 256 if its phase is 1, 512 if it is the right half of 128 columns; less than 0: no more
+    int valid;                // rows
+    const uint32_t* words;    // of an 8-bit tile: its rows' scale words; null: only rows behind the last are cleared
+};
 
 // An item that this CTA is to join: all of its threads do, when its part of the line is done.  (Four finishing warps on their own, with two or four
 // loads in flight, took up to 9 us.)
@@ -101,7 +102,6 @@ struct RgCtrl {
     int abort, count[kRgSegs / 32], units[kMaxSlots], entry[kMaxSlots];
     int first[kRgSegs], len[kRgSegs], piece[kRgSegs], pre[kRgSegs + 1];
     uint8_t slot[2][kRgSegs];
-    alignas(16) uint32_t words[kRgMaxStages][kRgWords];
     float4 turned[kRgFinish][32][5];
 };
 
@@ -213,7 +213,7 @@ __device__ __forceinline__ void rg_setup(RgCtrl* c, int warp, int tid, uint32_t 
         c->n_joins = 0;
         c->used_half[0] = c->used_half[1] = 0u;
         for (int i = 0; i < kRgMaxStages; ++i) {
-            mbar_init(smem_u32(&c->full[i]), 2);       // (tile and words: all that the converting warps wait for)
+            mbar_init(smem_u32(&c->full[i]), 1);
             mbar_init(smem_u32(&c->low_full[i]), 1);
             mbar_init(smem_u32(&c->empty[i]), 1);
         }
@@ -255,30 +255,13 @@ struct RgCursor {
 };
 __device__ __forceinline__ uint32_t turn_phase(int turn) { return (uint32_t)(turn / kRgTurns) & 1u; }
 
-// Producer of scale words (one thread): hands a stage on to the converting warps; stage -1: there is no more.
-__device__ __forceinline__ void post_turn(RgCtrl* c, int turn, int stage, uint32_t phase)
+// Producer of tiles (one thread): hands a stage on to the converting warps; stage -1: there is no more.
+__device__ __forceinline__ void post_turn(RgCtrl* c, int turn, const RgTurn& what)
 {
-    c->turns[turn % kRgTurns] = {stage, (int)phase};
+    c->turns[turn % kRgTurns] = what;
     mbar_arrive(smem_u32(&c->turn[turn % kRgTurns]));   // (releases what was written)
 }
-// ... the words of half a step's rows into the stage, from `words` on.  A bulk copy wants 16-byte boundaries, so it begins up to three words
-// early, and takes so many more.  That reaches into the rows behind and the next groups of columns, and with few rows behind the array's
-// end (10 rows: 13 groups on): then ordinary loads bring what does not fill 16 bytes.
-template <bool SECOND>
-__device__ __forceinline__ void load_words(RgCtrl* c, int stage, const uint32_t* words, const uint32_t* words_end)
-{
-    constexpr int kWords = SECOND ? 72 : kRgWords;
-    const uint32_t bar = smem_u32(&c->full[stage]);
-    const uint32_t* from = reinterpret_cast<const uint32_t*>(reinterpret_cast<uintptr_t>(words) & ~(uintptr_t)15);
-    uint32_t bytes = kWords * 4;
-    if (words_end - from < kWords) {
-        bytes = (uint32_t)(words_end - from) * 4u & ~15u;
-        for (const uint32_t* w = from + bytes / 4; w < words_end; ++w) c->words[stage][w - from] = ld_after_wait(w);
-    }
-    mbar_arrive_expect_tx(bar, bytes);
-    if (bytes) bulk_load(smem_u32(c->words[stage]), from, bytes, bar);
-}
-// Producer of tiles (one thread): the half step at (row, column) into the stage.
+// ... the half step at (row, column) into the stage.
 template <bool SECOND>
 __device__ __forceinline__ void load_tile(RgCtrl* c, const CUtensorMap* map, uint32_t at, int stage, bool raw, int row, int column)
 {
@@ -338,6 +321,12 @@ __device__ __forceinline__ void issue_steps(RgCtrl* c, const RgRing& ring, uint3
     } while (!(flags & kRgEnd));
 }
 
+// mbar_wait_warp where the barrier has turned as a rule: the lanes look for themselves first (one of them for all: 151 us for 145).
+__device__ __forceinline__ bool mbar_look_warp(uint32_t bar, uint32_t parity, volatile int* abort)
+{
+    return __all_sync(0xffffffffu, mbar_test_wait(bar, parity)) || mbar_wait_warp(bar, parity, abort);
+}
+
 // Converting group of both passes: the half steps that are handed on, in turn.  In the second pass rows behind the last become zeros (in a bf16
 // tile those that share a step of 16 with it: another token's values times zero would be NaN where they are not finite).
 template <bool E4M3, bool SECOND>
@@ -349,18 +338,37 @@ __device__ __forceinline__ void convert_tiles(RgCtrl* c, const RgRing& ring, int
     constexpr int kRows = (SECOND ? 4 : 8) * kRgGroup, kParts = (SECOND ? 64 : 128) / kRows;
     const int ch = wt & 3, odd = SECOND ? (wt >> 2) & 1 : 0, row0 = SECOND ? wt >> 3 : wt >> 2;
     const uint32_t to0 = (uint32_t)(odd * kRgHalfTile + row0 * 128 + (((2 * ch + odd) ^ (row0 & 7)) * 16));
+    // The scale words come straight from memory, and for the tile after this one as soon as it has been handed on, so that they are there with
+    // it as a rule.  (Copied into the stage by a producer of their own, 1000 tokens took 36.2 us for 34.8; asked for behind the conversion
+    // instead of before it, 8192 take 179 for 144.)
+    int where = 0, valid = 0;
+    bool raw = false;
+    uint32_t word[kParts];
+    const auto take = [&](int turn) {
+        const uint4 w = ld_smem_v4(smem_u32(&c->turns[turn % kRgTurns]));
+        where = (int)w.x;
+        valid = (int)w.y;
+        const uint32_t* words = reinterpret_cast<const uint32_t*>((uintptr_t)w.w << 32 | w.z);
+        raw = words != nullptr;
+#pragma unroll
+        for (int q = 0; q < kParts; ++q) word[q] = raw && row0 + kRows * q < valid ? ld_after_wait(words + row0 + kRows * q) : 0u;
+    };
+    bool taken = false;
     for (int turn = group;; turn += kRgGroups) {
         const int k = turn % kRgTurns;
-        bool ok = mbar_wait_warp(smem_u32(&c->turn[k]), turn_phase(turn), abort);
+        bool ok = true;
+        if (!taken) {
+            ok = mbar_look_warp(smem_u32(&c->turn[k]), turn_phase(turn), abort);
+            __syncwarp();
+            take(turn);
+        }
+        ok = ok && where >= 0;
+        const int stage = where & 255, rows_there = valid;
+        const bool kept = raw;
+        ok = ok && mbar_look_warp(smem_u32(&c->full[where < 0 ? 0 : stage]), (uint32_t)(where >> 8) & 1u, abort);
         __syncwarp();
-        const RgTurn what = c->turns[k];
-        ok = ok && what.stage >= 0;
-        const int stage = what.stage < 0 ? 0 : what.stage;
-        ok = ok && mbar_wait_warp(smem_u32(&c->full[stage]), (uint32_t)what.phase, abort);
-        __syncwarp();
-        const uint32_t at = ring.base + (uint32_t)stage * ring.stage_bytes;
-        const RgInfo info = c->info[stage];
-        const int shift = 8 * (SECOND ? (wt & 7) >> 1 : (ch >> 1) + (info.flags & kRgRight ? 2 : 0));
+        const uint32_t at = ring.base + (where < 0 ? 0u : (uint32_t)stage * ring.stage_bytes);
+        const int shift = 8 * (SECOND ? (wt & 7) >> 1 : (ch >> 1) + (where >> 8 & 2));
         uint2 v[kParts][2];
         uint32_t byte[kParts], most = 0;
 #pragma unroll
@@ -368,23 +376,25 @@ __device__ __forceinline__ void convert_tiles(RgCtrl* c, const RgRing& ring, int
             const uint4 w = ld_smem_v4(at + (uint32_t)(kRgTile - kRgRaw + q * (kRgRaw / kParts) + wt * 16));
             v[q][0] = odd ? make_uint2(w.z, w.w) : make_uint2(w.x, w.y);
             v[q][1] = odd ? make_uint2(w.x, w.y) : make_uint2(w.z, w.w);
-            byte[q] = (c->words[stage][(info.word & 3) + row0 + kRows * q] >> shift) & 0xffu;
+            byte[q] = (word[q] >> shift) & 0xffu;
             most = max(most, byte[q]);
         }
-        const bool usual = (!SECOND || info.valid == 64) && most <= Decoder<E4M3>::kMost;
+        const bool usual = (!SECOND || rows_there == 64) && most <= Decoder<E4M3>::kMost;
         if (group_any(group, !ok)) return;   // (everybody has the tile's values, so their place may be written; or there is no more, or a wait gave up)
+        taken = __all_sync(0xffffffffu, mbar_test_wait(smem_u32(&c->turn[(turn + kRgGroups) % kRgTurns]), turn_phase(turn + kRgGroups)));
+        if (taken) take(turn + kRgGroups);
         const uint32_t to = at + to0;
-        if (info.word >= 0 && usual) {
+        if (kept && usual) {
 #pragma unroll
             for (int q = 0; q < kParts; ++q) {
                 const Decoder<E4M3> decode(byte[q]);
                 st_smem_v4(to + (uint32_t)(q * kRows * 128), decode.eight(v[q][0]));
                 st_smem_v4((to ^ 16u) + (uint32_t)(q * kRows * 128), decode.eight(v[q][1]));
             }
-        } else if (info.word >= 0) {
+        } else if (kept) {
 #pragma unroll 1
             for (int q = 0; q < kParts; ++q) {
-                const bool there = !SECOND || row0 + kRows * q < info.valid;
+                const bool there = !SECOND || row0 + kRows * q < rows_there;
                 const uint4 zero = make_uint4(0, 0, 0, 0);
                 st_smem_v4(to + (uint32_t)(q * kRows * 128), there ? decode8<E4M3>(v[0][0], byte[0]) : zero);
                 st_smem_v4((to ^ 16u) + (uint32_t)(q * kRows * 128), there ? decode8<E4M3>(v[0][1], byte[0]) : zero);
@@ -392,9 +402,9 @@ __device__ __forceinline__ void convert_tiles(RgCtrl* c, const RgRing& ring, int
                 for (int i = 0; i + 1 < kParts; ++i) { v[i][0] = v[i + 1][0]; v[i][1] = v[i + 1][1]; byte[i] = byte[i + 1]; }
             }
         } else if (SECOND) {
-            const int rows = 16 - (info.valid & 15);
+            const int rows = 16 - (rows_there & 15);
             for (int e = wt; e < rows * 16; e += 32 * kRgGroup) {
-                const int row = info.valid + (e >> 4);
+                const int row = rows_there + (e >> 4);
                 st_smem_v4(at + ((e >> 3) & 1) * kRgHalfTile + row * 128 + (e & 7) * 16, make_uint4(0, 0, 0, 0));
             }
         }
@@ -579,20 +589,26 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_shrink_kernel(const __grid
         if (warp == 0) {
             if (elect_one()) {
                 const CUtensorMap* map = nullptr;
+                const uint32_t* words = nullptr;
                 bool raw = false;
                 int r16 = 0, valid = 0, row = 0;
-                uint32_t words_at = 0;   // in words of four bytes; what counts is where they lie to 16
-                each([&](const ShrinkTasks& t) {
+                const int turns = each([&](const ShrinkTasks& t) {
                          map = &p.map[0][t.job]; row = t.row; valid = t.valid;
                          r16 = chunks_of_rank(p.snap[t.job].rank[t.slot]) * kChunk;
                          raw = FMT != kBf16 && t.job == 0;
-                         words_at = (uint32_t)(reinterpret_cast<uintptr_t>(p.scales) >> 2) + (uint32_t)t.row;
+                         words = p.scales + t.row + (size_t)t.step * p.T;
                      },
                      [&](RgCursor& u, int k, int half, int last) {
-                         const int flags = last | (raw ? kRgTouched : 0) | (half ? kRgRight : 0);
-                         c->info[u.stage] = {flags, valid, r16, raw ? (int)((words_at + (uint32_t)(k >> 7) * (uint32_t)p.T) & 3u) : -1};
+                         c->info[u.stage] = {last | (raw ? kRgTouched : 0), valid, r16};
                          load_tile<false>(c, map, u.at, u.stage, raw, row, k + 64 * half);
+                         if (raw) {
+                             post_turn(c, u.turn, {u.stage | (int)u.phase << 8 | half << 9, valid, words});
+                             ++u.turn;
+                             if (half) words += p.T;   // (a step with one half is the last)
+                         }
                      });
+                if (FMT != kBf16)
+                    for (int k = 0; k < kRgGroups; ++k) post_turn(c, turns + k, {-1, 0, nullptr});
             }
         } else if (warp == kRgOther) {
             if (elect_one()) {
@@ -608,27 +624,6 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_shrink_kernel(const __grid
                          mbar_arrive_expect_tx(bar, bytes);
                          tma_load_2d(u.at + kRgTile, map, bar, k + 64 * half, row);
                      });
-            }
-        } else if (warp == kRgWordsWarp) {
-            if (elect_one()) {
-                const uint32_t *words = nullptr, *words_end = p.scales + (size_t)kept_groups(p.d[0]) * p.T;
-                bool raw = false;
-                const int turns = each([&](const ShrinkTasks& t) {
-                        raw = FMT != kBf16 && t.job == 0;
-                        words = p.scales + t.row + (size_t)t.step * p.T;
-                    },
-                    [&](RgCursor& u, int, int half, int) {
-                        if (!raw) {
-                            mbar_arrive(smem_u32(&c->full[u.stage]));
-                        } else {
-                            load_words<false>(c, u.stage, words, words_end);
-                            if (half) words += p.T;   // (a step with one half is the last)
-                            post_turn(c, u.turn, u.stage, u.phase);
-                            ++u.turn;
-                        }
-                    });
-                if (FMT != kBf16)
-                    for (int k = 0; k < kRgGroups; ++k) post_turn(c, turns + k, -1, 0);
             }
         } else if (warp == 1) {
             if (elect_one()) issue_steps<false>(c, ring, tmem, (uint32_t)p.r16, abort);
@@ -869,18 +864,24 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_grad_kernel(const __grid_c
         if (warp == 0) {
             if (elect_one()) {
                 const CUtensorMap* map = nullptr;
+                const uint32_t* words = nullptr;
                 bool is_raw = false;
                 int column = 0, r16 = 0;
-                uint32_t words_at = 0;
-                each([&](const GradTasks& t, bool raw) {
+                const int turns = each([&](const GradTasks& t, bool raw) {
                          map = &p.map[1][t.job()]; is_raw = raw; column = t.column();
                          r16 = chunks_of_rank(p.snap[0].rank[t.slot]) * kChunk;
-                         words_at = (uint32_t)(reinterpret_cast<uintptr_t>(p.scales) >> 2) + (uint32_t)t.tile * (uint32_t)p.T;
+                         words = p.scales + (size_t)t.tile * p.T;
                      },
                      [&](RgCursor& u, const RgPieces& v, int half, int rows, int flags) {
-                         c->info[u.stage] = {flags, rows, r16, is_raw ? (int)((words_at + (uint32_t)v.row()) & 3u) : -1};   // (64 rows on it is the same)
-                         load_tile<true>(c, map, u.at, u.stage, is_raw, v.row() + 64 * half, column);
+                         const int row = v.row() + 64 * half;
+                         c->info[u.stage] = {flags, rows, r16};
+                         load_tile<true>(c, map, u.at, u.stage, is_raw, row, column);
+                         if (flags & kRgTouched) {
+                             post_turn(c, u.turn, {u.stage | (int)u.phase << 8, rows, is_raw ? words + row : nullptr});
+                             ++u.turn;
+                         }
                      });
+                for (int k = 0; k < kRgGroups; ++k) post_turn(c, turns + k, {-1, 0, nullptr});
             }
         } else if (warp == kRgOther) {
             if (elect_one()) {
@@ -897,18 +898,6 @@ __global__ void __launch_bounds__(kRgThreads, 1) rows_grad_kernel(const __grid_c
                          mbar_arrive_expect_tx(bar, low);
                          bulk_load(u.at + kRgTile, pieces + v.at() + half * low, low, bar);
                      });
-            }
-        } else if (warp == kRgWordsWarp) {
-            if (elect_one()) {
-                const uint32_t *words = nullptr, *words_end = p.scales + (size_t)kept_groups(p.d[0]) * p.T;
-                bool is_raw = false;
-                const int turns = each([&](const GradTasks& t, bool raw) { is_raw = raw; words = p.scales + (size_t)t.tile * p.T; },
-                    [&](RgCursor& u, const RgPieces& v, int half, int, int flags) {
-                        if (is_raw) load_words<true>(c, u.stage, words + v.row() + 64 * half, words_end);
-                        else mbar_arrive(smem_u32(&c->full[u.stage]));
-                        if (flags & kRgTouched) { post_turn(c, u.turn, u.stage, u.phase); ++u.turn; }
-                    });
-                for (int k = 0; k < kRgGroups; ++k) post_turn(c, turns + k, -1, 0);
             }
         } else if (warp == 1) {
             if (elect_one()) issue_steps<true>(c, ring, tmem, 3u * (uint32_t)p.r16, abort);
@@ -1057,7 +1046,7 @@ __global__ void __launch_bounds__(1024) rows_check_kernel(const int32_t* seg_off
 }
 
 // ---- host ---------------------------------------------------------------------------------------------
-constexpr int kRgRing = 203 * 1024;   // one CTA to an SM
+constexpr int kRgRing = 208 * 1024;   // one CTA to an SM
 
 // Workspace: [u][v][partial results of both passes' CTAs][whether the arrays hold together]
 struct RgLayout { size_t pieces, partial, bad, total; };

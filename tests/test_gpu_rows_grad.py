@@ -121,7 +121,7 @@ def test_gradients(T, K, N, ranks, lengths, seg_entry, form):
 @pytest.mark.parametrize("T,lengths", [(1, [1, 0]), (10, [7, 3]), (70, [66, 4]), (137, [3, 134])])
 @pytest.mark.parametrize("K", (368, 4096))
 def test_scale_words_that_end_where_the_memory_ends(T, lengths, K):
-    """The words of a tile's rows come in whole pieces of 16 bytes, more than there are rows; nothing behind the array may be read."""
+    """A tile has 128 rows and the array of scale words ends with the last row of the batch; nothing behind it may be read."""
     import torch
     from paper_2608_15241_b200 import binding as b
     c = Case(T, K, 264, [16, 33], lengths, [0, 1])
