@@ -38,7 +38,7 @@ namespace lml {
 
 using namespace ptx;
 
-constexpr int kRgGroups = 2, kRgGroup = 8;      // converting groups, warps of each
+constexpr int kRgGroups = 4, kRgGroup = 4;     // converting groups, warps of each
 constexpr int kRgFinish = 4;                    // warps that finish items (warps 2 ... 5: one per quarter of the accumulator's lanes)
 constexpr int kRgOther = 2 + kRgFinish;         // the warp that brings in the other operand
 constexpr int kRgFirstConv = kRgOther + 1;
