@@ -26,9 +26,9 @@
 // value, side by side as 3r columns of one product.  One bf16 value would leave 2^-9, 1e-3 of every gradient, two 3e-6.
 //
 // x and dy leave HBM once (the second pass finds them in L2 up to about 100 MB), but memory is not what bounds it: 8192 x 11008 in E4M3 and 4096,
-// eight adapters of 8 to 64 ranks, take 144 us where the bytes take 28.  It is the way of a stage through its ring, load, conversion, product and
-// back, some 4000 cycles; no role is busy for more than half of the time, and without the conversion it is 11 % less, without the other
-// operand 1 %, without the tiles' loads 8 %.  Small calls (100 tokens of one adapter 16 us) are made of a dozen such latencies in a row.
+// eight adapters of 8 to 64 ranks, take 138 us where the bytes take 28.  It is the way of a stage through its ring, load, conversion, product and
+// back, some 4000 cycles; no role is busy for more than half of the time, and without the conversion it is 12 % less, without the other
+// operand 1 %, without the tiles' loads 5 %.  Small calls (100 tokens of one adapter 16 us) are made of a dozen such latencies in a row.
 #include <cstring>
 
 #include "lml_ptx_sm100.cuh"
@@ -38,7 +38,7 @@ namespace lml {
 
 using namespace ptx;
 
-constexpr int kRgGroups = 4, kRgGroup = 4;     // converting groups, warps of each
+constexpr int kRgGroups = 4, kRgGroup = 4;      // converting groups, warps of each (8192 tokens, below: 138 us; two of eight 143, one of sixteen 208, eight of two 161)
 constexpr int kRgFinish = 4;                    // warps that finish items (warps 2 ... 5: one per quarter of the accumulator's lanes)
 constexpr int kRgOther = 2 + kRgFinish;         // the warp that brings in the other operand
 constexpr int kRgFirstConv = kRgOther + 1;
