@@ -435,6 +435,13 @@ def _stream_on(device: int, stream) -> int:
     return _raw_stream_of(device)
 
 
+def _with_stream(stream):
+    """For a call that allocates: the given stream as the current one, so that what it allocates (results and, above all, a workspace that nobody
+    holds when the call returns) is that stream's memory."""
+    import torch
+    return torch.cuda.stream(stream)
+
+
 def _bf16_rows(t, shape, name, device: int) -> int:
     """Checks a bf16 [T][d] tensor of a call on cuda:`device` and gives its address; None is 0."""
     if t is None:
@@ -534,21 +541,27 @@ class Checkpoint:
     def load(self, out=None, stream=None):
         """The values it stands for, bf16 [tokens][width]."""
         import torch
+        if stream is not None:
+            with _with_stream(stream):
+                return self.load(out)
         shape, dev = (self.tokens, self.width), self.device
         if out is None:
             out = (self._data if self._data is not None else self._buffer).new_empty(shape, dtype=torch.bfloat16)
             at = out.data_ptr()
         else:
             at = _bf16_rows(out, shape, "out", dev)
-        lml_checkpoint_load(dev, self.rows, self.tokens, self.width, at, _stream_on(dev, stream))
+        lml_checkpoint_load(dev, self.rows, self.tokens, self.width, at, _stream_on(dev, None))
         return out
 
 
 def checkpoint_store(x, form: str = "int8", stream=None) -> Checkpoint:
     """A new checkpoint of x (bf16 [T][d])."""
     import torch
+    if stream is not None:
+        with _with_stream(stream):
+            return checkpoint_store(x, form)
     T, d = x.shape
-    return Checkpoint._in(x.new_empty(Checkpoint._bytes(T, d), dtype=torch.uint8), T, d, form).store(x, stream)
+    return Checkpoint._in(x.new_empty(Checkpoint._bytes(T, d), dtype=torch.uint8), T, d, form).store(x)
 
 
 def _as_rows(x, shape, name, device: int):
@@ -580,6 +593,9 @@ class BlockNorm:
         """-> (h', x).  o None: h' is h.  gate_rows: a gate per token, bf16 [T][d].  h_new / x: where to write them (new tensors otherwise);
         x_checkpoint / h_checkpoint: Checkpoints that the same pass fills.  x is None without w_pre."""
         import torch
+        if stream is not None:
+            with _with_stream(stream):
+                return self.forward(h, o, gate_rows, h_new, x, x_checkpoint, h_checkpoint)
         T, dev = int(h.shape[0]), _cuda_index(h, "h")
         shape = (T, self.d)
         assert self.device is None or dev == self.device, dev
@@ -595,7 +611,7 @@ class BlockNorm:
         else:
             x_at = _bf16_rows(x, shape, "x", dev)
         lml_block_norm(dev, self.desc, T, h_at, _bf16_rows(o, shape, "o", dev), _bf16_rows(gate_rows, shape, "gate_rows", dev), h_new_at, x_at,
-                       _as_rows(x_checkpoint, shape, "x_checkpoint", dev), _as_rows(h_checkpoint, shape, "h_checkpoint", dev), _stream_on(dev, stream))
+                       _as_rows(x_checkpoint, shape, "x_checkpoint", dev), _as_rows(h_checkpoint, shape, "h_checkpoint", dev), _stream_on(dev, None))
         return (h if o is None else h_new), x
 
     def backward(self, h_new, o, dx, dh_new, gate_rows=None, dh=None, d_o=None, dw_pre=None, dw_post=None, dgate=None, workspace=None,
@@ -604,6 +620,9 @@ class BlockNorm:
         dw_pre, dw_post, dgate: float32 [d] that the sums over the tokens are added to, or None (frozen).  The third result is dgate, or with
         gate_rows their gradient, bf16 [T][d]."""
         import torch
+        if stream is not None:
+            with _with_stream(stream):
+                return self.backward(h_new, o, dx, dh_new, gate_rows, dh, d_o, dw_pre, dw_post, dgate, workspace)
         some = dx if dx is not None else dh_new
         T, d, dev = int(some.shape[0]), self.d, _cuda_index(some, "dx")
         shape = (T, d)
@@ -631,7 +650,7 @@ class BlockNorm:
                 n_ws = workspace.numel() * workspace.element_size()
         lml_block_norm_backward(dev, self.desc, T, _as_rows(h_new, shape, "h_new", dev), _as_rows(o, shape, "o", dev), gate_at, dx_at, dh_new_at,
                                 dh_at, d_o_at, _sums(dw_pre, (d,), "dw_pre", dev), _sums(dw_post, (d,), "dw_post", dev),
-                                _sums(dgate, (d,), "dgate", dev), _ptr(dgate_rows), _ptr(workspace) if n_ws else 0, n_ws, _stream_on(dev, stream))
+                                _sums(dgate, (d,), "dgate", dev), _ptr(dgate_rows), _ptr(workspace) if n_ws else 0, n_ws, _stream_on(dev, None))
         return dh, d_o, (dgate_rows if gate_rows is not None else dgate)
 
 
@@ -799,6 +818,9 @@ class Table:
         """backward_adapters with x as a Checkpoint (or a bf16 tensor) and unrounded small products.  accumulate=False: the rows j < rank of
         every live slot are written, so that dA and dB need not be zeroed before a step's first batch."""
         import torch
+        if stream is not None:
+            with _with_stream(stream):
+                return self.backward_adapters_rows(table_T, x, dy, seg_offsets, slot_ids, slot_ids_T, dA, dB, accumulate, workspace)
         T, G, dev = int(dy.shape[0]), int(slot_ids.shape[0]), self.device
         assert dA.dtype is torch.float32 and dB.dtype is torch.float32 and dA.is_contiguous() and dB.is_contiguous()
         assert dA.shape == (self.max_slots, 64, self.d_in) and dB.shape == (self.max_slots, self.d_out, 64)
@@ -814,7 +836,7 @@ class Table:
         lora_mixed_linear_backward_adapters_rows(self.handle, table_T.handle, _as_rows(x, (T, self.d_in), "x", dev), dy_at, T,
                                                  seg_offsets.data_ptr(), slot_ids.data_ptr(), slot_ids_T.data_ptr(), G, dA.data_ptr(),
                                                  dB.data_ptr(), accumulate, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                                                 _stream_on(dev, stream))
+                                                 _stream_on(dev, None))
 
     def lora_mixed_linear_dual(self, x, W0, seg_offsets, slot_ids_a, slot_ids_b, perm=None, stream=None):
         """-> (y_a, y_b): the layer under two slot bindings of the same segments."""

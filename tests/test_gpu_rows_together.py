@@ -75,3 +75,42 @@ def test_a_training_step_of_one_projection():
         assert rel(dA[e, :ranks[e]].cpu().numpy(), exact[e][0]) <= 2.0 ** -6 and rel(dB[e, :, :ranks[e]].cpu().numpy(), exact[e][1]) <= 2.0 ** -6
     t.close()
     tT.close()
+
+
+def test_memory_of_calls_on_a_stream_that_is_behind():
+    """Calls on a stream of their own that has other work to do first; meanwhile the current stream asks for memory and writes to it."""
+    import torch
+    from paper_2608_15241_b200.binding import BlockNorm, Table, checkpoint_store
+    T, d, r = 300, 512, 16
+    g = torch.Generator(device="cuda").manual_seed(5)
+    mk = lambda *s: torch.randn(*s, generator=g, device="cuda").to(torch.bfloat16)  # noqa: E731
+    norm = BlockNorm(d, w_post=mk(d), w_pre=mk(d), gate=mk(d), scale=0.5)
+    h, o, dx, dh = (mk(T, d) for _ in range(4))
+    t, tT = Table(d, d, 2), Table(d, d, 2)
+    A, B = mk(r, d), mk(d, r)
+    ids, ids_T = t.register_adapter(0, 1, A, B, 1.0), tT.register_adapter_transposed(0, 1, A, B, 1.0)
+    dev = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    so, ids, ids_T = dev([0, T]), dev([ids]), dev([ids_T])
+
+    def step(stream):
+        sums = torch.zeros((3, d), device="cuda")
+        dA, dB = torch.zeros((2, 64, d), device="cuda"), torch.zeros((2, d, 64), device="cuda")
+        torch.cuda.synchronize()
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                torch.cuda._sleep(20_000_000)
+        h_new, x = norm.forward(h, o, stream=stream)
+        kept = checkpoint_store(x, "int8", stream=stream)
+        back = kept.load(stream=stream)
+        gh, go, _ = norm.backward(h_new, o, dx, dh, dw_pre=sums[0], dw_post=sums[1], dgate=sums[2], stream=stream)
+        t.backward_adapters_rows(tT, kept, dh, so, ids, ids_T, dA, dB, accumulate=False, stream=stream)
+        junk = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in (1 << k for k in range(9, 24)) for _ in range(3)]
+        torch.cuda.synchronize()
+        del junk
+        return h_new, x, back, gh, go, sums, dA, dB
+
+    want, got = step(None), step(torch.cuda.Stream())
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
+    t.close()
+    tT.close()
