@@ -312,13 +312,14 @@ lml_status lml_checkpoint_load(int device, const lml_rows* kept, int T, int d, v
  * as in lora_mixed_linear_backward_adapters, with x the values that the rows stand for.  On the tensor cores; the two small products are
  * fp32 and stay so on the way (three bf16 values each instead of one), so dA and dB are sums in fp32 of products that are not rounded.  The
  * order of the sums is fixed by the sizes, the segments and the bindings: the same call gives the same bits.  Two launches for every 320
- * segments (and one more where there are more than that); a call of no tokens has one.
+ * segments (one while t holds no adapter), and one more where there are more than that; a call of no tokens has one, or none.
  * accumulate != 0: rows j < rank of the slots in use are added to.  accumulate == 0: rows j < rank of EVERY live slot of t are
  * written, zeros where the batch has no token of it (a step's first micro-batch then needs no zeroed buffers).  Rows j >= rank
  * and slots without an adapter are left as they are either way.
  * A segment takes part when its two slots hold adapters of one rank; one that names only one of them, a free slot or another
- * rank adds nothing and sets LML_FLAG_BAD_SLOT (of t_T where t's slot is fine).  Malformed seg_offsets: LML_FLAG_BAD_OFFSETS,
- * nothing is added.  A token's Inf or NaN reaches the gradients of its own adapter only.
+ * rank adds nothing and sets LML_FLAG_BAD_SLOT: of t where t's slot holds no adapter, of t_T where its slot's rank is not that of t's
+ * (no adapter: rank 0).  Malformed seg_offsets: LML_FLAG_BAD_OFFSETS of t, nothing is added.  A token's Inf or NaN reaches the
+ * gradients of its own adapter only.
  * x, dy: rows in segment order (no perm), 16-byte aligned.  G >= 1.  dA, dB must not overlap x or dy.
  * The CTAs that share an item count themselves in words of the table t: two calls on the SAME table must not overlap on the GPU, put
  * them on one stream or order them.

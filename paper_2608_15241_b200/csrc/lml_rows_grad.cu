@@ -1079,7 +1079,7 @@ cudaError_t launch_rows_grad(const RowsGradCall& a, cudaStream_t stream, int* la
 {
     RowsGradParams p;
     *launches = 0;
-    int most = 0, live = 0;
+    int most = 1, live = 0;
     p.live = 0ull;
     p.snap[0] = *a.snap; p.snap[1] = *a.snap_T;
     for (int s = 0; s < a.snap->max_slots; ++s)
@@ -1088,7 +1088,7 @@ cudaError_t launch_rows_grad(const RowsGradCall& a, cudaStream_t stream, int* la
             p.live |= 1ull << s;
             ++live;
         }
-    if (live == 0) return cudaSuccess;
+    if (live == 0 && a.T == 0) return cudaSuccess;
     p.r16 = chunks_of_rank(most) * kChunk;
     const RgLayout lay = rg_layout(a.T, a.G, a.num_sms);
     uint8_t* ws = static_cast<uint8_t*>(a.workspace);
@@ -1153,6 +1153,7 @@ cudaError_t launch_rows_grad(const RowsGradCall& a, cudaStream_t stream, int* la
         const long long pieces = a.T / kTileM + p.G;   // at most: every segment can have one that is not full
         cudaError_t e = launch(shrink, pieces * p.all_tiles / kRgLeast);
         if (e != cudaSuccess) return e;
+        if (live == 0) continue;   // (nothing to write; the first pass has looked at the segments all the same)
         // Few pieces to an item: whole items, unless there are so many that their number leaves CTAs idle at the end.
         const int slots = p.G < live ? p.G : live;
         const long long items = (long long)p.all_tiles * slots;
