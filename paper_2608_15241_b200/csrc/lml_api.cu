@@ -248,7 +248,7 @@ lml_status lml_table_create(lml_table** out, int device, int d_in, int d_out, in
     ok = ok && cudaMemset(t->arena.adapter_map, 0xff, kMaxAdapterIds * sizeof(int32_t)) == cudaSuccess;   // -1: no serving version
     ok = ok && cudaMalloc(&t->arena.pass_flags, kFuseMaxPasses * sizeof(int32_t)) == cudaSuccess;
     ok = ok && cudaMemset(t->arena.pass_flags, 0, kFuseMaxPasses * sizeof(int32_t)) == cudaSuccess;
-    const size_t arrived_bytes = (size_t)t->num_sms * 2 * sizeof(int32_t);
+    const size_t arrived_bytes = (size_t)t->num_sms * 2 * sizeof(uint32_t);
     ok = ok && cudaMalloc(&t->arena.rows_arrived, arrived_bytes) == cudaSuccess;
     ok = ok && cudaMemset(t->arena.rows_arrived, 0, arrived_bytes) == cudaSuccess;
     ok = ok && decode_init() == cudaSuccess;   // (first: see there)
@@ -1148,7 +1148,7 @@ lml_status lml_device_status(lml_table* t, uint32_t* flags_out, void* stream_v)
         // a launch gave up on a wait: its counters may have been left behind, so the decode kernel's exchange blocks
         // start over (only then: in normal operation nothing here touches memory that a call in flight uses)
         ok = cudaMemsetAsync(t->arena.status + 8, 0, 2 * sizeof(uint32_t), stream) == cudaSuccess;
-        ok = ok && cudaMemsetAsync(t->arena.rows_arrived, 0, (size_t)t->num_sms * 2 * sizeof(int32_t), stream) == cudaSuccess;
+        ok = ok && cudaMemsetAsync(t->arena.rows_arrived, 0, (size_t)t->num_sms * 2 * sizeof(uint32_t), stream) == cudaSuccess;
         ok = ok && cudaMemsetAsync(t->arena.dec_u, 0, (size_t)kDecMaxBlocks * kDecExchStride * sizeof(unsigned long long), stream) == cudaSuccess;
         ok = ok && cudaStreamSynchronize(stream) == cudaSuccess;
     }

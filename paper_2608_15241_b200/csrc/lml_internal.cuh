@@ -50,7 +50,7 @@ struct Arena {
     uint32_t* status;   // sticky LML_FLAG_* bits
     int32_t* pass_flags;    // [kFuseMaxPasses] fused shrink of the prefill GEMM: the u blocks of pass i are written (= epoch + 1; the epoch is word 4 of status)
     int32_t* adapter_map;   // [kMaxAdapterIds] serving entry of each adapter id: slot | generation << 8, -1 = none; written by lml_publish
-    int32_t* rows_arrived;   // [2][SM] gradients from rows, of each pass: CTAs that have left their part of a shared item
+    uint32_t* rows_arrived;   // [2][SM] gradients from rows, of each pass: CTAs that have left their part of a shared item; zero between calls
     unsigned long long* dec_u;   // [kDecMaxBlocks][kDecExchStride] the decode kernel's exchange blocks, one per part of a launch that works on this table
 };
 

@@ -65,7 +65,9 @@ struct alignas(64) RowsGradParams {
     uint32_t* status[2];
     uint8_t* pieces[2];       // u, v
     float* partial;           // [CTA][2]: of the item that its part begins in, of the item that its part ends in
-    int* arrived[2];          // [CTA], of each pass: of the item that its part ends in and the next one goes on with; the other pass clears them
+    // [CTA], of each pass: of the item that its part ends in and the next one goes on with.  The last to arrive sets it back to 0, so that a call cut
+    // off between its launches leaves nothing; and each pass clears the other's, so that calls that overlapped leave nothing to a third.
+    unsigned* arrived[2];
     float* out[2];            // dA, dB
     int d[2], tiles[2];       // d_in, d_out; in tiles of 128 columns
     int T, G, num_sms, r16, ring, accumulate, all_tiles, whole_items;
@@ -429,12 +431,13 @@ __device__ __forceinline__ RgShare share_of(const RgLine& line, int item, int n,
     return {first, line.part_of(item + n - 1), k == first ? 1 : 0};   // (the others begin behind the item's first step)
 }
 // After all finishing warps have written this CTA's partial result: if it is the last one of the item's, the CTA joins them later.
-__device__ __forceinline__ void arrive(RgCtrl* c, int* arrived, const RgShare& s, int job, int slot, int at, int valid)
+__device__ __forceinline__ void arrive(RgCtrl* c, unsigned* arrived, const RgShare& s, int job, int slot, int at, int valid)
 {
     __threadfence();
     finish_barrier();
     if (threadIdx.x == 64) {   // (the first of them)
-        if (atomicAdd(arrived + s.first, 1) == s.last - s.first) c->joins[c->n_joins++] = {job, slot, s.first, s.last, at, valid};
+        const unsigned others = (unsigned)(s.last - s.first);
+        if (atomicInc(arrived + s.first, others) == others) c->joins[c->n_joins++] = {job, slot, s.first, s.last, at, valid};
         __threadfence();
     }
 }

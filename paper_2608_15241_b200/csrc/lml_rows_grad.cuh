@@ -15,7 +15,7 @@ struct RowsGradCall {
     const int32_t *seg_offsets, *ids, *ids_T;
     float *dA, *dB;
     void* workspace;
-    int32_t* arrived;   // of the table: a counter per CTA, zero between calls
+    uint32_t* arrived;   // of the table: a counter per CTA and pass, zero between calls
     int T, G, d_in, d_out, num_sms;
     bool accumulate;
 };
