@@ -319,7 +319,7 @@ lml_status lml_checkpoint_load(int device, const lml_rows* kept, int T, int d, v
  * A segment takes part when its two slots hold adapters of one rank; one that names only one of them, a free slot or another
  * rank adds nothing and sets LML_FLAG_BAD_SLOT: of t where t's slot holds no adapter, of t_T where its slot's rank is not that of t's
  * (no adapter: rank 0).  Malformed seg_offsets: LML_FLAG_BAD_OFFSETS of t, nothing is added.  A token's Inf or NaN reaches the
- * gradients of its own adapter only.
+ * gradients of its own adapter only; sums that have infinite terms are what IEEE makes of them.
  * x, dy: rows in segment order (no perm), 16-byte aligned.  G >= 1.  dA, dB must not overlap x or dy.
  * The CTAs that share an item count themselves in words of the table t: two calls on the SAME table must not overlap on the GPU, put
  * them on one stream or order them.

@@ -148,7 +148,12 @@ __device__ __forceinline__ void chunk_sums(uint32_t from, uint32_t r16, uint32_t
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         s[e] = __uint_as_float(h[e]);
-        if (PARTS == 3) s[e] += __uint_as_float(m[e]) + __uint_as_float(l[e]);
+        if (PARTS == 3) {
+            // A token's Inf times the lower parts may be NaN (they are zero as often as not) or an Inf of the other sign: the first part says it all.
+            // (100 tokens: 15.7 -> 16.0 us.  A look at all eight for NaN instead, with what follows apart, spills: 16.3.)
+            const float sum = s[e] + (__uint_as_float(m[e]) + __uint_as_float(l[e]));
+            s[e] = fabsf(s[e]) < INFINITY ? sum : s[e];
+        }
         if (more) s[e] += __uint_as_float(before[e]);
     }
 }
