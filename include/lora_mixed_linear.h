@@ -367,7 +367,8 @@ lml_status lml_block_norm(int device, const lml_block_norm_desc* desc, int T, co
  * h_new may be NULL without dx, o NULL where the forward call had none (then d_o, dw_post, dgate, dgate_rows are NULL).
  * An output NULL is not made.  Buffers may be shared as above (dh = dh_new, d_o = dx, say).  Sums over tokens are added in an order that
  * T and d fix.  One launch, two where sums are wanted; those need workspace: lml_block_norm_workspace_bytes(device, T, d), 256-byte aligned.
- * Errors: INVALID_ARG, WORKSPACE, CUDA.
+ * There is no table here to hold a status word: should a wait for a row inside the kernel run out (about a second), what would have
+ * come of the row is NaN, and so are the sums.  Errors: INVALID_ARG, WORKSPACE, CUDA.
  */
 size_t lml_block_norm_workspace_bytes(int device, int T, int d);
 lml_status lml_block_norm_backward(int device, const lml_block_norm_desc* desc, int T, const lml_rows* h_new, const lml_rows* o,

@@ -11,6 +11,7 @@
 // A group of W warps holds a row in registers, V vectors of eight columns per thread, so every tensor is read and written
 // once: bound by memory.
 #include <atomic>
+#include <cstdlib>
 #include <type_traits>
 
 #include "lml_rows.cuh"
@@ -150,10 +151,11 @@ __global__ void __launch_bounds__(NormShape<W>::kWarps * 32) block_norm_kernel(c
 // What bounds it next to memory is the number of instructions and the wait at a row's sums.  So a row has one meeting of its warps: with
 // z = a g w_post o, the mean that do asks for is that of D z = dh' z + rho dx w_pre z - rho^2 mean(..) h' z, three more sums next to those of
 // h'^2, o^2 and dx w_pre h', all six added across the warps in one go.  Arithmetic is on pairs of columns; a thread's columns of the weights and,
-// with one vector per thread, of the row stay in registers.  (Loading into registers: 317 us where this takes 111, 8192 x 5120
-// from E4M3 checkpoints, 3.7 TB/s; with copies ahead but decoding in every phase 185; two meetings per row 150, two rows at a time 153; the
+// with one vector per thread, of the row stay in registers.  What happens when a wait gives up stands behind the loop over rows, which then needs
+// no registers for it.  (8192 x 5120 from E4M3 checkpoints: 96 us, 4.4 TB/s; 110 with a question about the wait at every vector.  On the way there,
+// loading into registers 317, with copies ahead but decoding in every phase 185, two meetings per row 150, two rows at a time 153, the
 // copies on one thread 141.)
-constexpr int kNormSmem = 160 * 1024;   // five rows of 5120; what is left of the SM's is L1, for the few spills (224 KB: 117 us for 111)
+constexpr int kNormSmem = 160 * 1024;   // five rows of 5120; what is left of the SM's is L1, for the spills that there were (224 KB: 117 us where 160 took 111)
 constexpr int kNormStages = 64;
 __host__ __device__ constexpr int norm_warps(int V) { return V == 1 ? 20 : 16; }   // of a CTA, at most: 96 or 128 registers per thread
 
@@ -161,6 +163,7 @@ struct NormBackwardLaunch {
     NormBackward a;
     int W, G, stages, stage_bytes;       // stages: of a group
     int at_dh, at_h, at_o, at_gate, at_words;   // in a stage; dx comes first
+    int waited_for;                      // rows that are: all (with LML_NORM_PATIENCE=0 none)
 };
 
 // Arrives at the barrier when the words that this thread has asked for are there.
@@ -354,11 +357,11 @@ __global__ void __launch_bounds__(32 * norm_warps(V), 1) block_norm_backward_ker
     const size_t where_step = (size_t)step * d;
     int stage = 0, turn = 0;
     uint32_t phase = 0;
-    for (unsigned t = first; t < (unsigned)T; t += step, turn ^= 1, where0 += where_step) {
+    unsigned t = first;
+    for (; t < (unsigned)L.waited_for; t += step, turn ^= 1, where0 += where_step) {
         const uint8_t* at = ring + (size_t)stage * L.stage_bytes;
         const uint32_t* wh = reinterpret_cast<const uint32_t*>(at + L.at_words);
-        const bool arrived = mbar_try_wait(smem_u32(&bars[stage]), phase) || mbar_wait(smem_u32(&bars[stage]), phase, &gave_up);
-        __syncwarp();
+        if (!__all_sync(0xffffffffu, mbar_try_wait(smem_u32(&bars[stage]), phase) || mbar_wait(smem_u32(&bars[stage]), phase, &gave_up))) break;
         // h'^2, o^2, dx w_pre h' (mean(dx w_pre hh) = rho mean(dx w_pre h')), and dh', dx w_pre and h' by z
         Eight<kPacked> hp[V], op[V];
         Eight<true> gp[V], qp[V];
@@ -381,7 +384,6 @@ __global__ void __launch_bounds__(32 * norm_warps(V), 1) block_norm_backward_ker
             else op[i].set(zero);
             if (has_dh_new && ok) ld_stage(qp[i], at + L.at_dh, vec, kBf16, nullptr);
             else qp[i].set(zero);
-            if (!arrived) qp[i].set(make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u));   // (a wait gave up: its results are NaN)
             float2 h[4], g[4], o[4], q[4], w[4], gate[4];
             hp[i].get(h); gp[i].get(g); op[i].get(o); qp[i].get(q); w_pre[i].get(w);
             if (row_gate) unpack_pairs(ok ? *reinterpret_cast<const uint4*>(at + L.at_gate + vec * 16) : zero, gate);
@@ -465,10 +467,35 @@ __global__ void __launch_bounds__(32 * norm_warps(V), 1) block_norm_backward_ker
         }
         if (++stage == L.stages) { stage = 0; phase ^= 1u; }
     }
+    if (t < (unsigned)T) {
+        // A wait gave up.  Of this row and all that follow this warp makes NaN, of the sums too, and through the meeting the others do.  It asks for
+        // no more rows: copies that have not landed may still count on the stages' barriers, whose phases nobody knows any more.
+        const float nan = __uint_as_float(0x7fc00000u);
+        const uint4 nans = make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
+#pragma unroll 1
+        for (; t < (unsigned)T; t += step, turn ^= 1, where0 += where_step) {
+            if (lane < 6) red[turn][group * W + mine][lane] = nan;
+            group_barrier();
+            for (int i = 0; i < V; ++i) {
+                const int vec = i * W * 32 + in;
+                const size_t where = where0 + i * W * 256;
+                if (!kAll && vec >= vecs) continue;
+                if (wants_dh) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.dh) + where) = nans;
+                if (wants_do) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.d_o) + where) = nans;
+                if (row_gate && a.dgate_rows) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.dgate_rows) + where) = nans;
+            }
+            if (row_gate) group_barrier();
+        }
+        if (SUMS) {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s_pre[i][e] = s_o[i][e] = both(nan);
+        }
+        __nanosleep(50000);   // let copies still in flight land before their place is used again, by this CTA or the next
+    }
     if (!SUMS) return;
     // this CTA's partial sums, groups added in order, where the ring was
-    __syncwarp();
-    if (gave_up) __nanosleep(50000);
     __syncthreads();
     float* sums = reinterpret_cast<float*>(norm_smem);
     float* out = a.partial + (size_t)blockIdx.x * 2 * d;
@@ -624,6 +651,16 @@ static cudaError_t norm_init()   // once per device
     return e;
 }
 
+// LML_NORM_PATIENCE=0 (as it stands at the first call; a test knob): no row is waited for, as if every wait had given up.
+static bool norm_waits()
+{
+    static const bool waits = [] {
+        const char* e = getenv("LML_NORM_PATIENCE");
+        return !e || atoi(e) > 0;
+    }();
+    return waits;
+}
+
 cudaError_t launch_block_norm_backward(const NormBackward& a, int num_sms, cudaStream_t stream)
 {
     cudaError_t e = norm_init();
@@ -632,6 +669,7 @@ cudaError_t launch_block_norm_backward(const NormBackward& a, int num_sms, cudaS
     const int d = a.n.d, vecs = d / 8, ctas = norm_backward_ctas(a.n.T, num_sms), rows = (a.n.T + ctas - 1) / ctas;   // of a CTA
     NormBackwardLaunch L;
     L.a = a;
+    L.waited_for = norm_waits() ? a.n.T : 0;
     // One vector per thread up to the width that the warps allow; two or four where a row is wider.
     const int V = vecs <= 32 * norm_warps(1) ? 1 : vecs <= 2 * 32 * norm_warps(2) ? 2 : 4;
     L.W = (vecs + 32 * V - 1) / (32 * V);
