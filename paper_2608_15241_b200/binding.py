@@ -435,10 +435,12 @@ def _stream_on(device: int, stream) -> int:
     return _raw_stream_of(device)
 
 
-def _with_stream(stream):
+def _with_stream(stream, device: int):
     """For a call that allocates: the given stream as the current one, so that what it allocates (results and, above all, a workspace that nobody
-    holds when the call returns) is that stream's memory."""
+    holds when the call returns) is that stream's memory.  A stream of another device than the tensors' is refused: the call would run on the
+    current stream of theirs."""
     import torch
+    assert stream.device.index == device, ("stream", stream.device, device)
     return torch.cuda.stream(stream)
 
 
@@ -542,7 +544,7 @@ class Checkpoint:
         """The values it stands for, bf16 [tokens][width]."""
         import torch
         if stream is not None:
-            with _with_stream(stream):
+            with _with_stream(stream, self.device):
                 return self.load(out)
         shape, dev = (self.tokens, self.width), self.device
         if out is None:
@@ -558,7 +560,7 @@ def checkpoint_store(x, form: str = "int8", stream=None) -> Checkpoint:
     """A new checkpoint of x (bf16 [T][d])."""
     import torch
     if stream is not None:
-        with _with_stream(stream):
+        with _with_stream(stream, _cuda_index(x, "x")):
             return checkpoint_store(x, form)
     T, d = x.shape
     return Checkpoint._in(x.new_empty(Checkpoint._bytes(T, d), dtype=torch.uint8), T, d, form).store(x)
@@ -594,7 +596,7 @@ class BlockNorm:
         x_checkpoint / h_checkpoint: Checkpoints that the same pass fills.  x is None without w_pre."""
         import torch
         if stream is not None:
-            with _with_stream(stream):
+            with _with_stream(stream, _cuda_index(h, "h")):
                 return self.forward(h, o, gate_rows, h_new, x, x_checkpoint, h_checkpoint)
         T, dev = int(h.shape[0]), _cuda_index(h, "h")
         shape = (T, self.d)
@@ -620,10 +622,10 @@ class BlockNorm:
         dw_pre, dw_post, dgate: float32 [d] that the sums over the tokens are added to, or None (frozen).  The third result is dgate, or with
         gate_rows their gradient, bf16 [T][d]."""
         import torch
-        if stream is not None:
-            with _with_stream(stream):
-                return self.backward(h_new, o, dx, dh_new, gate_rows, dh, d_o, dw_pre, dw_post, dgate, workspace)
         some = dx if dx is not None else dh_new
+        if stream is not None:
+            with _with_stream(stream, _cuda_index(some, "dx")):
+                return self.backward(h_new, o, dx, dh_new, gate_rows, dh, d_o, dw_pre, dw_post, dgate, workspace)
         T, d, dev = int(some.shape[0]), self.d, _cuda_index(some, "dx")
         shape = (T, d)
         assert self.device is None or dev == self.device, dev
@@ -819,7 +821,7 @@ class Table:
         every live slot are written, so that dA and dB need not be zeroed before a step's first batch."""
         import torch
         if stream is not None:
-            with _with_stream(stream):
+            with _with_stream(stream, self.device):
                 return self.backward_adapters_rows(table_T, x, dy, seg_offsets, slot_ids, slot_ids_T, dA, dB, accumulate, workspace)
         T, G, dev = int(dy.shape[0]), int(slot_ids.shape[0]), self.device
         assert dA.dtype is torch.float32 and dB.dtype is torch.float32 and dA.is_contiguous() and dB.is_contiguous()

@@ -1,0 +1,42 @@
+"""Host-only checks of the binding's row calls: what they refuse before anything is allocated or launched."""
+from types import SimpleNamespace
+
+import pytest
+
+from paper_2608_15241_b200 import binding
+
+
+class OnDevice:
+    """As much of a CUDA tensor as a call looks at before it refuses a stream."""
+    is_cuda, shape = True, (4, 64)
+
+    def __init__(self, index):
+        self.index = index
+
+    def get_device(self):
+        return self.index
+
+
+def _stream(index):
+    import torch
+    return SimpleNamespace(device=torch.device("cuda", index), device_index=index, cuda_stream=0x10)
+
+
+def _calls():
+    kept = binding.Checkpoint.__new__(binding.Checkpoint)
+    kept.device = 0
+    table = binding.Table.__new__(binding.Table)
+    table.device, table.handle = 0, 0
+    norm, t = binding.BlockNorm(64), OnDevice(0)
+    yield "load", lambda s: kept.load(stream=s)
+    yield "store", lambda s: binding.checkpoint_store(t, stream=s)
+    yield "forward", lambda s: norm.forward(t, stream=s)
+    yield "backward", lambda s: norm.backward(None, t, None, t, stream=s)
+    yield "backward", lambda s: norm.backward(t, None, t, None, stream=s)
+    yield "gradients", lambda s: table.backward_adapters_rows(None, t, t, None, None, None, None, None, stream=s)
+
+
+@pytest.mark.parametrize("name,call", list(_calls()))
+def test_a_stream_of_another_device_is_refused(name, call):
+    with pytest.raises(AssertionError, match="stream"):
+        call(_stream(1))
