@@ -11,6 +11,7 @@ retire_version, lml_segment_tokens, lora_mixed_linear, ...) and take raw pointer
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 from typing import Optional, Tuple
 
@@ -580,13 +581,16 @@ class BlockNorm:
     """The norms between two blocks (lml_block_norm): weights and gate bf16 [d] or None, kept by the caller's program.
 
         n = rmsnorm(o) w_post;  h' = h + scale gate n;  x = rmsnorm(h') w_pre
+
+    The weights may be written to, but not replaced: the descriptor holds their addresses.
     """
+    d, w_post, w_pre, gate, scale, eps = (property(operator.attrgetter("_" + name)) for name in ("d", "w_post", "w_pre", "gate", "scale", "eps"))
 
     def __init__(self, d: int, w_post=None, w_pre=None, gate=None, scale: float = 1.0, eps: float = 1e-5):
         import torch
         for name, w in (("w_post", w_post), ("w_pre", w_pre), ("gate", gate)):
             assert w is None or (w.dtype == torch.bfloat16 and w.is_cuda and w.is_contiguous() and tuple(w.shape) == (d,)), name
-        self.d, self.w_post, self.w_pre, self.gate, self.scale, self.eps = d, w_post, w_pre, gate, float(scale), float(eps)
+        self._d, self._w_post, self._w_pre, self._gate, self._scale, self._eps = d, w_post, w_pre, gate, float(scale), float(eps)
         self.device = next((w.get_device() for w in (w_post, w_pre, gate) if w is not None), None)
         assert all(w is None or w.get_device() == self.device for w in (w_post, w_pre, gate)), "weights on several devices"
         self.desc = BlockNormDesc(d, eps, scale, _ptr(w_post), _ptr(w_pre), _ptr(gate))

@@ -40,3 +40,14 @@ def _calls():
 def test_a_stream_of_another_device_is_refused(name, call):
     with pytest.raises(AssertionError, match="stream"):
         call(_stream(1))
+
+
+def test_a_norm_keeps_what_it_was_made_of():
+    """Its descriptor holds the weights' addresses: a weight, a scale or an eps put in their place would be ignored, and the memory of the weight that
+    it drops read all the same."""
+    norm = binding.BlockNorm(64, scale=0.5, eps=1e-3)
+    for name, value in (("w_post", OnDevice(0)), ("w_pre", OnDevice(0)), ("gate", OnDevice(0)), ("scale", 2.0), ("eps", 1e-6), ("d", 128)):
+        with pytest.raises(AttributeError):
+            setattr(norm, name, value)
+    assert (norm.d, norm.scale, norm.eps, norm.w_post, norm.w_pre, norm.gate) == (64, 0.5, 1e-3, None, None, None)
+    assert (norm.desc.d, norm.desc.scale) == (64, 0.5) and not norm.desc.w_pre
