@@ -49,8 +49,9 @@ template <int W> struct NormShape {
 
 // W: warps of a row (a number that is known here: 22.4 us for 8192 x 4096 where one that is not took 25).  AHEAD: the weights are asked for along
 // with the row.
+// Four vectors per thread: 64 registers at most, 32 warps on an SM.
 template <int W, int V, bool AHEAD>
-__global__ void __launch_bounds__(NormShape<W>::kWarps * 32) block_norm_kernel(const __grid_constant__ NormForward a)
+__global__ void __launch_bounds__(NormShape<W>::kWarps * 32, V == 4 && !AHEAD ? 32 / NormShape<W>::kWarps : 1) block_norm_kernel(const __grid_constant__ NormForward a)
 {
     __shared__ float red[2][NormShape<W>::kWarps];
     ptx::grid_dependency_wait();
