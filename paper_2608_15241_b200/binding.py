@@ -533,6 +533,7 @@ class Checkpoint:
         return self._scales
 
     def nbytes(self) -> int:
+        """Device memory that it takes."""
         return self._bytes(self.tokens, self.width)
 
     def store(self, x, stream=None) -> "Checkpoint":
@@ -588,6 +589,7 @@ class BlockNorm:
 
     def __init__(self, d: int, w_post=None, w_pre=None, gate=None, scale: float = 1.0, eps: float = 1e-5):
         import torch
+        assert 0 < d <= MAX_NORM_WIDTH and d % 8 == 0, d
         for name, w in (("w_post", w_post), ("w_pre", w_pre), ("gate", gate)):
             assert w is None or (w.dtype == torch.bfloat16 and w.is_cuda and w.is_contiguous() and tuple(w.shape) == (d,)), name
         self._d, self._w_post, self._w_pre, self._gate, self._scale, self._eps = d, w_post, w_pre, gate, float(scale), float(eps)

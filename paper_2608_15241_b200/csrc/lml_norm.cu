@@ -47,8 +47,8 @@ template <int W> struct NormShape {
     static constexpr int kGroups = W > 8 ? 1 : 8 / W, kWarps = W * kGroups;
 };
 
-// W: warps of a row (a number that is known here: 22.4 us for 8192 x 4096 where one that is not took 25).  AHEAD: the weights are asked for along
-// with the row.
+// W: warps of a row (a number that the compiler knows takes a tenth less than one that it does not, 8192 x 4096).  AHEAD: the weights are asked for
+// along with the row.
 // Four vectors per thread: 64 registers at most, 32 warps on an SM.
 template <int W, int V, bool AHEAD>
 __global__ void __launch_bounds__(NormShape<W>::kWarps * 32, V == 4 && !AHEAD ? 32 / NormShape<W>::kWarps : 1) block_norm_kernel(const __grid_constant__ NormForward a)
@@ -253,8 +253,8 @@ __device__ __forceinline__ float warp_sums6(const float (&s)[6], int lane)
 }
 
 // V: vectors of a row per thread.  FMT >= 0: the usual call, all of whose inputs and outputs but a gate per token are there, o and h'
-// in this format, and whose threads' vectors make up the row: nothing to ask about at every step (what is asked about otherwise
-// takes two fifths of the instructions).
+// in this format, and whose threads' vectors make up the row: nothing to ask about at every step (8192 x 5120 in bf16 81 us, 6.2 TB/s; the
+// others: 8192 x 2880 120 us, 2.4 TB/s, 8192 x 4096 with a gate per token 164 us, 3.3 TB/s).
 template <int V, bool SUMS, int FMT>
 __global__ void __launch_bounds__(32 * norm_warps(V), 1) block_norm_backward_kernel(const __grid_constant__ NormBackwardLaunch L)
 {
@@ -586,11 +586,11 @@ __global__ void __launch_bounds__(32 * kSumSlices) norm_sums_kernel(const __grid
 cudaError_t launch_block_norm(const NormForward& a, int num_sms, cudaStream_t stream)
 {
     // As few vectors per thread as the warps allow where there are rows for one wave at most: what counts is one row's time.  Two for more, to
-    // some 40 rows per SM (2000 x 4096 with all that there is: 12.3 us, four 14.7; 3000 x 4096 17.3 and 19.5), four beyond, where
-    // what counts is loads in flight (8192 x 4096 without o: 22.4 us, 6.0 TB/s, two 24.7; 16384 x 2048 21.7 and 27.1).  The weights are asked
-    // for ahead of the sums up to a few waves (40 x 4096 with a gate per token: 2.5 us, 3.4 behind them); beyond they come from L1, and the
-    // registers are better used for more rows (8192 x 4096: 26.4 us with two vectors, 29.8 ahead).  T and d decide and nothing else: a call on h'
-    // alone gives the same bits.
+    // some 40 rows per SM (2000 x 4096 with a block before: 15.6 us, four 17.1; 3000 x 4096 21.2 and 21.8), four beyond, where what counts
+    // is loads in flight (8192 x 4096 without o: 24.1 us, 5.6 TB/s, two 29.8; 16384 x 2048 23.1 and 29.0; 5000 x 4096 with a block before the same).
+    // The weights are asked for ahead of the sums up to a few waves (40 x 4096 with a gate per token: 2.4 us, 2.8 behind them; 1000 x 4096 9.4 and
+    // 10.0); beyond they come from L1, and the registers are better used for more rows (8192 x 4096 without o: 24.1 us, 34.0 ahead).  T and d decide
+    // and nothing else: a call on h' alone gives the same bits.
     const int vecs = a.n.d / 8;
     const bool ahead = a.n.T <= 8 * num_sms;
     int V = a.n.T <= num_sms ? 1 : a.n.T <= 40 * num_sms ? 2 : 4;
@@ -604,6 +604,8 @@ cudaError_t launch_block_norm(const NormForward& a, int num_sms, cudaStream_t st
         pdl_config(cfg, attr, dim3((unsigned)(((long long)a.n.T + kGroups - 1) / kGroups)), dim3(NormShape<W>::kWarps * 32), 0, stream);
         return cudaLaunchKernelEx(&cfg, ahead ? block_norm_kernel<W, V, true> : block_norm_kernel<W, V, false>, a);
     };
+    // Numbers of warps that there are kernels for: powers of two, and 5 and 10 in their widest gaps, so that a third of a row's threads at most have
+    // nothing to do (11 warps' columns on 16).
     const auto widths = [&](auto v) {
         const auto fits = [&](auto w) { return needs <= decltype(w)::value; };
         using std::integral_constant;

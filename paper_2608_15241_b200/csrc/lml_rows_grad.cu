@@ -6,7 +6,7 @@
 // may begin at any row, so no row of another segment is in it but behind its end) of x or of dy, its work the steps of 128 columns.
 // rows_grad_kernel: dA and dB.  An item is (slot, 128 columns of x or dy), its work the slot's pieces.
 // A step of either is a tile of 128 rows x 128 columns, which goes through the rings in two halves along what is contracted: 64 columns in the
-// first pass, 64 rows in the second: a stage's way through loading, conversion and product is some 4000 cycles whatever its size, so
+// first pass, 64 rows in the second: a stage's way through loading, conversion and product takes about as long whatever its size, so
 // what counts is how many there are (beside 64 ranks eight and five; with the 8 bits in a place of their own six and four, and 5 % more time
 // for 8192 x 11008 in E4M3 and 4096).
 // In both the work of all items stands in one line that is cut into equal parts, one per SM; a CTA walks its part without a pause
@@ -26,9 +26,11 @@
 // value, side by side as 3r columns of one product.  One bf16 value would leave 2^-9, 1e-3 of every gradient, two 3e-6.
 //
 // x and dy leave HBM once (the second pass finds them in L2 up to about 100 MB), but memory is not what bounds it: 8192 x 11008 in E4M3 and 4096,
-// eight adapters of 8 to 64 ranks, take 138 us where the bytes take 28.  It is the way of a stage through its ring, load, conversion, product and
-// back, some 4000 cycles; no role is busy for more than half of the time, and without the conversion it is 12 % less, without the other
-// operand 1 %, without the tiles' loads 5 %.  Small calls (100 tokens of one adapter 16 us) are made of a dozen such latencies in a row.
+// eight adapters of 8 to 64 ranks, take 138 us where the bytes take 28, and nothing is saturated (tensor pipe 5 and 12 %, DRAM 28 %, half of the issue
+// slots).  A CTA has about 110 half steps in either pass, some 1100 and 1250 cycles each.  A stage takes 4000 to 6000 from empty to empty.  With five
+// of them that is what bounds the second pass; the first has eight, for which half steps of 750 would do: what holds it up has not been found.
+// (Without the conversion the call takes 12 % less, without the tiles' loads 5 %, without the other operand 1 %.)  Small calls (100 tokens of one
+// adapter 16 us) are made of a dozen latencies in a row.
 #include <cstring>
 
 #include "lml_ptx_sm100.cuh"

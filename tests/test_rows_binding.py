@@ -51,3 +51,19 @@ def test_a_norm_keeps_what_it_was_made_of():
             setattr(norm, name, value)
     assert (norm.d, norm.scale, norm.eps, norm.w_post, norm.w_pre, norm.gate) == (64, 0.5, 1e-3, None, None, None)
     assert (norm.desc.d, norm.desc.scale) == (64, 0.5) and not norm.desc.w_pre
+
+
+def test_widths_that_no_call_takes():
+    for d in (0, -8, 12, 16392):
+        with pytest.raises(AssertionError):
+            binding.BlockNorm(d)
+    assert binding.BlockNorm(binding.MAX_NORM_WIDTH).d == 16384
+
+
+def test_what_a_checkpoint_takes():
+    from paper_2608_15241_b200 import build
+    build.build()
+    for T, d in ((0, 8), (1, 8), (5, 4104), (300, 136), (8192, 11008)):
+        kept = binding.Checkpoint.__new__(binding.Checkpoint)
+        kept.tokens, kept.width = T, d
+        assert kept.nbytes() == binding.lml_checkpoint_data_bytes(T, d) + binding.lml_checkpoint_scale_bytes(T, d)
