@@ -49,9 +49,10 @@ template <int W> struct NormShape {
 
 // W: warps of a row (a number that the compiler knows takes a tenth less than one that it does not, 8192 x 4096).  AHEAD: the weights are asked for
 // along with the row.
-// Four vectors per thread: 64 registers at most, 32 warps on an SM.
+// Four vectors per thread: 64 registers at most, 32 warps on an SM.  (Nothing is asked of the other kernels, with one CTA asked for
+// they take a third more registers.)
 template <int W, int V, bool AHEAD>
-__global__ void __launch_bounds__(NormShape<W>::kWarps * 32, V == 4 && !AHEAD ? 32 / NormShape<W>::kWarps : 1) block_norm_kernel(const __grid_constant__ NormForward a)
+__global__ void __launch_bounds__(NormShape<W>::kWarps * 32, V == 4 && !AHEAD ? 32 / NormShape<W>::kWarps : 0) block_norm_kernel(const __grid_constant__ NormForward a)
 {
     __shared__ float red[2][NormShape<W>::kWarps];
     ptx::grid_dependency_wait();
@@ -586,10 +587,10 @@ __global__ void __launch_bounds__(32 * kSumSlices) norm_sums_kernel(const __grid
 cudaError_t launch_block_norm(const NormForward& a, int num_sms, cudaStream_t stream)
 {
     // As few vectors per thread as the warps allow where there are rows for one wave at most: what counts is one row's time.  Two for more, to
-    // some 40 rows per SM (2000 x 4096 with a block before: 15.6 us, four 17.1; 3000 x 4096 21.2 and 21.8), four beyond, where what counts
-    // is loads in flight (8192 x 4096 without o: 24.1 us, 5.6 TB/s, two 29.8; 16384 x 2048 23.1 and 29.0; 5000 x 4096 with a block before the same).
-    // The weights are asked for ahead of the sums up to a few waves (40 x 4096 with a gate per token: 2.4 us, 2.8 behind them; 1000 x 4096 9.4 and
-    // 10.0); beyond they come from L1, and the registers are better used for more rows (8192 x 4096 without o: 24.1 us, 34.0 ahead).  T and d decide
+    // some 40 rows per SM (2000 x 4096 with a block before: 14.9 us, four 17.1; 5000 x 4096 30.4 and 32.0), four beyond, where what counts is
+    // loads in flight (8192 x 4096 without o: 24.2 us, 5.6 TB/s, two 27.1; 16384 x 2048 23.2 and 29.4; 8192 x 4096 with a block before the same).
+    // The weights are asked for ahead of the sums up to a few waves (40 x 4096 with a gate per token: 2.4 us, 2.8 behind them; 1000 x 4096 8.8 and
+    // 10.0); beyond they come from L1, and the registers are better used for more rows (8192 x 4096 without o: 24.2 us, 41 ahead).  T and d decide
     // and nothing else: a call on h' alone gives the same bits.
     const int vecs = a.n.d / 8;
     const bool ahead = a.n.T <= 8 * num_sms;
